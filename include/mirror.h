@@ -309,6 +309,93 @@ mirror_status mirror_kv_commit_fp8(mirror_ctx* ctx, const mirror_kv* kv, const m
                                    const void* v_new_fp8, const int32_t* accepted_nodes, const int32_t* n_accepted,
                                    int32_t* prefix_len, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Tokens that are no tree: prompts, and single tokens decoded without a draft (the prefix that a verify step builds on).
+ * ------------------------------------------------------------------------------------------------------------ */
+/* New rows of several requests, one behind the other.  Row i of request b sits at position kv->prefix_len[b] + i, where
+ * prefix_len counts the tokens that the cache held before these rows (no call here changes it). */
+typedef struct {
+    int batch;                /* B requests, at most 1024 */
+    int n_rows;               /* R: rows of the tensors, those behind the last request's included (they are left as they are) */
+    int max_rows;             /* upper bound of a request's rows; 1: single tokens */
+    const int32_t* row_start; /* device [B + 1], not decreasing: request b has the rows row_start[b] .. row_start[b+1] - 1;
+                                 NULL: every request has max_rows rows (R >= B * max_rows) */
+} mirror_rows;
+
+typedef enum {
+    MIRROR_ROPE_PLAIN = 0,    /* f_i = theta^(-2i / rotary_dim) radians per position for pair i */
+    MIRROR_ROPE_LINEAR = 1,   /* f_i / factor: positions pressed together evenly */
+    MIRROR_ROPE_TURNS = 2,    /* w f_i + (1 - w) f_i / factor, w = clamp((t_i - low) / (high - low), 0, 1): t_i = original_len f_i / 2 pi is
+                                 how often pair i turned over the lengths seen in training */
+    MIRROR_ROPE_PAIRS = 3     /* the same blend, linear in the pair's index: with i(t) = rotary_dim ln(original_len / (2 pi t)) / (2 ln theta),
+                                 a = max(floor(i(high)), 0), b = min(ceil(i(low)), rotary_dim - 1): w = 1 - clamp((i - a) / max(b - a, 0.001), 0, 1) */
+} mirror_rope_scaling;
+
+/* A rotation of the first rotary_dim elements of a head (the others pass through): pair i turns by position * f_i.  Pairs are
+ * (i, i + rotary_dim / 2), or (2i, 2i + 1) when interleaved.  Filled by mirror_rope_init. */
+typedef struct {
+    int rotary_dim;
+    int interleaved;
+    double amplitude;         /* factor on cos and sin */
+    double freq[64];          /* f_i */
+} mirror_rope;
+
+/* HOST helper (no device work): the frequencies above, in double precision.
+ *   head_dim 64 or 128; rotary_dim a multiple of 16 up to head_dim (0: head_dim); theta > 1
+ *   factor, original_len, low < high (turns): read by the scalings that name them; amplitude > 0 (0 selects 1) */
+mirror_status mirror_rope_init(mirror_rope* out, int head_dim, int rotary_dim, int interleaved, double theta,
+                               mirror_rope_scaling scaling, double factor, double original_len, double low, double high,
+                               double amplitude);
+
+/* Append to the paged cache: keys turned to their positions, values as they are; the queries are turned on the way.
+ *   kv        k_pool / v_pool are WRITTEN (the struct's const is not honoured by this call); page_table must hold pages for the
+ *             new positions; prefix_len: tokens before the rows
+ *   rope      HOST, NULL: no rotation
+ *   q         bf16 [L, R, Hq, d], nullable; k, v  bf16 [L, R, Hkv, d].  Heads and elements are contiguous; rows are q_row / kv_row
+ *             elements apart and layers q_layer / kv_layer (so the three may be columns of one projection's output); all of
+ *             them multiples of 8
+ *   q_out     bf16 [L, R, Hq, d], contiguous, nullable (with q); may be q where that is contiguous
+ * Angles are reduced in double precision, the rotation is fp32 with one rounding.  Two rows must not share a (page, slot).  A position
+ * beyond max_pages_per_req*16 or below 0, or a page outside the pool, is skipped and reported through mirror_device_status.
+ * One kernel. */
+mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, const mirror_rows* rows, const mirror_rope* rope,
+                               const void* q, int64_t q_row, int64_t q_layer, void* q_out, const void* k, const void* v,
+                               int64_t kv_row, int64_t kv_layer, void* stream);
+
+/* Causal attention of the rows over the paged cache, their own keys and values included (mirror_kv_append comes first): the
+ * row at position p sees token j <= p iff window == 0, or j > p - window, or j < n_sink ("sinks": first tokens that stay
+ * visible).
+ *   q, out    bf16 [L, R, Hq, d] contiguous (q already turned): out = softmax(scale q k^T over the visible tokens) v
+ *   lse_out   fp32 [L, R, Hq], nullable: natural-log softmax denominator
+ * Pages that hold no visible token are not touched (their table entries may be anything), and what lies in a touched page beside
+ * the tokens that some row of its request sees may be anything, infinities and NaN included.
+ * Needs a workspace of mirror_rows_workspace_bytes().  Requests of few rows for now: max_rows * Hq / Hkv <= 16
+ * (MIRROR_ERR_UNSUPPORTED otherwise). */
+mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, const mirror_rows* rows, size_t* bytes);
+mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mirror_rows* rows, int window, int n_sink,
+                                 const void* q, void* out, float* lse_out, void* stream);
+
+/* One token of every row of logits, from a given uniform, under filters:
+ *   logits      fp32 [M, V], rows `ld` elements apart (V of the ctx)
+ *   temperature fp32 [M], nullable (the ctx's): a row with T <= 0 keeps only its first maximum
+ *   top_k       int32 [M], nullable: the top_k largest logits stay, of equals the lower ids (<= 0 or >= V: off)
+ *   top_p       fp32 [M], nullable: of what is left, the shortest front of the ranks whose share of the probability reaches
+ *               top_p: a token stays iff those ahead of it have less (>= 1: off; <= 0: the first alone)
+ *   min_p       fp32 [M], nullable: tokens with at least min_p times the largest probability stay (<= 0: off)
+ *   u           fp32 [M] in [0, 1): the token is the first id at which the kept tokens' probabilities, summed over ids in
+ *               increasing order, exceed u (inverse CDF, as in mirror_accept_select)
+ *   token       int32 [M]; logprob fp32 [M], nullable: ln of its probability among the kept; n_kept int32 [M], nullable
+ *   probs       fp32 [M, V], nullable: the kept tokens' probabilities, 0 elsewhere -- q_probs of mirror_accept_in for a draft
+ *   logits_out  fp32 [M, V], nullable: T_ctx * ln of them, -inf elsewhere -- with an lse of zeros, the logits that
+ *               mirror_accept_select takes for a target under the same filters
+ * All three filters keep a front of the ranks (logit descending, id ascending), at least the first.  NaN logits are never kept (a row without
+ * any other: token -1, logprob -inf, n_kept 0, probs 0), -inf only where top_k reaches them, never drawn; logits of +inf share all the mass.
+ * Weights exp((logit - max) / T) are summed as 64-bit integers, scaled to 2^62 / V: sums are the same in any order.
+ * One kernel, no workspace. */
+mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int64_t ld, int M, const float* temperature,
+                            const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token,
+                            float* logprob, int32_t* n_kept, float* probs, float* logits_out, void* stream);
+
 /* HOST helper (no device work): merge kappa branches of gamma tokens -- the branch-complete proposal of Sec. 3.1 --
  * into a token tree without duplicated prefixes ("tree drafts"): branches that agree on their first r tokens share
  * their first r nodes, so shared tokens are scored once.  All pointers are HOST pointers.

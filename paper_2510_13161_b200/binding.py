@@ -28,10 +28,11 @@ EXPORTS = [
     "mirror_lmhead_reduce_noalloc", "mirror_lmhead_noalloc_status", "mirror_quantize_rows_fp8", "mirror_lmhead_reduce_fp8", "mirror_early_exit_tap", "mirror_overlap_mass", "mirror_kv_commit",
     "mirror_linear_scratch_bytes", "mirror_linear", "mirror_rmsnorm", "mirror_target_scratch_bytes", "mirror_target_forward", "mirror_trie_build", "mirror_verify_step_host", "mirror_embed_rows",
     "mirror_attn_verify_fp8", "mirror_kv_scales_fp8", "mirror_kv_quantize_fp8", "mirror_kv_commit_fp8", "mirror_verify_step_fp8", "mirror_target_forward_fp8",
+    "mirror_rope_init", "mirror_kv_append", "mirror_rows_workspace_bytes", "mirror_attn_causal", "mirror_sample",
 ]
 
 
-# Argument types of the exports, one letter each: p pointer, i int, u unsigned, f float, z size_t, l int64.  (Declared, so that
+# Argument types of the exports, one letter each: p pointer, i int, u unsigned, f float, d double, z size_t, l int64.  (Declared, so that
 # plain Python integers can be passed for pointers: wrapping every argument costs more than the call.)
 _SIGNATURES = {
     "mirror_create": "ppi", "mirror_destroy": "p", "mirror_workspace_bytes": "pppup", "mirror_set_workspace": "ppz",
@@ -44,9 +45,10 @@ _SIGNATURES = {
     "mirror_embed_rows": "pppipp", "mirror_rmsnorm": "pppiifpp", "mirror_target_scratch_bytes": "pppp",
     "mirror_target_forward": "p" * 12 + "zp", "mirror_target_forward_fp8": "p" * 17 + "zp",
     "mirror_verify_step_fp8": "p" * 8 + "f" + "p" * 7, "mirror_verify_step_host": "p" * 17, "mirror_set_stage_events": "pp",
-    "mirror_device_status": "ppp", "mirror_launch_count": "pp",
+    "mirror_rope_init": "piiididdddd", "mirror_kv_append": "ppppp" + "ll" + "ppp" + "ll" + "p", "mirror_rows_workspace_bytes": "ppp",
+    "mirror_attn_causal": "pppiipppp", "mirror_sample": "ppli" + "p" * 11, "mirror_device_status": "ppp", "mirror_launch_count": "pp",
 }
-_CTYPES = {"p": C.c_void_p, "i": C.c_int, "u": C.c_uint, "f": C.c_float, "z": C.c_size_t, "l": C.c_int64}
+_CTYPES = {"p": C.c_void_p, "i": C.c_int, "u": C.c_uint, "f": C.c_float, "d": C.c_double, "z": C.c_size_t, "l": C.c_int64}
 
 
 class MirrorError(RuntimeError):
@@ -83,6 +85,17 @@ class KV(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("layer_stride", C.c_int64),
                 ("num_layers", C.c_int), ("num_pages", C.c_int), ("max_pages_per_req", C.c_int),
                 ("page_table", C.c_void_p), ("prefix_len", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("batch", C.c_int), ("n_rows", C.c_int), ("max_rows", C.c_int), ("row_start", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int), ("interleaved", C.c_int), ("amplitude", C.c_double), ("freq", C.c_double * 64)]
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "turns": 2, "pairs": 3}
 
 
 class AcceptIn(C.Structure):
@@ -432,6 +445,116 @@ class Mirror:
                                              _ptr(v_new8, torch.uint8, "v_new8"), _ptr(res.accepted_nodes, torch.int32, "accepted_nodes"),
                                              _ptr(res.n_accepted, torch.int32, "n_accepted"), _ptr(prefix_len, torch.int32, "prefix_len"),
                                              _stream(stream)), "mirror_kv_commit_fp8")
+
+    # ---- prompts and single tokens: rows of several requests, without a tree --------------------
+    def rows(self, row_start: Optional[torch.Tensor], n_rows: int, max_rows: int, batch: Optional[int] = None) -> Rows:
+        """Ragged rows: request b has the rows row_start[b] .. row_start[b+1] - 1 (int32 [B + 1]), at most max_rows of them.
+        row_start None: `batch` requests of max_rows rows each."""
+        if row_start is None:
+            if batch is None:
+                raise ValueError("batch is needed without row_start")
+        elif batch is not None and batch != row_start.numel() - 1:
+            raise ValueError("row_start must have batch + 1 entries")
+        r = Rows(batch if row_start is None else row_start.numel() - 1, n_rows, max_rows, _ptr(row_start, torch.int32, "row_start"))
+        r._refs = (row_start,)
+        return r
+
+    def rope(self, rotary_dim: int = 0, interleaved: bool = False, theta: float = 1e6, scaling: str = "none", factor: float = 1.0,
+             original_len: float = 0.0, low: float = 1.0, high: float = 32.0, amplitude: float = 1.0) -> Rope:
+        """Frequencies of the rotation (see mirror_rope_init): scaling none, linear, turns or pairs; rotary_dim 0: the whole head."""
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+        out = Rope()
+        _check(self.lib.mirror_rope_init(C.byref(out), self.desc.head_dim, rotary_dim, int(interleaved), theta, ROPE_SCALINGS[scaling],
+                                         factor, original_len, low, high, amplitude), "mirror_rope_init")
+        return out
+
+    def _strided(self, t: torch.Tensor, heads: int, rows: Rows, name: str):
+        """Address, row and layer stride of a bf16 tensor [L, R, heads, d] whose heads and elements are contiguous."""
+        d = self.desc.head_dim
+        if not t.is_cuda or t.dtype is not torch.bfloat16:
+            raise ValueError(f"{name} must be a CUDA tensor of torch.bfloat16")
+        if t.dim() != 4 or t.shape[1] != rows.n_rows or t.shape[2] != heads or t.shape[3] != d:
+            raise ValueError(f"{name} must be [L, {rows.n_rows}, {heads}, {d}], got {tuple(t.shape)}")
+        st = t.stride()
+        if st[3] != 1 or (heads > 1 and st[2] != d):
+            raise ValueError(f"{name}: heads and elements must be contiguous")
+        # (a stride of a dimension of one entry may be anything)
+        row = st[1] if t.shape[1] > 1 else heads * d
+        return t.data_ptr(), row, st[0] if t.shape[0] > 1 else row * t.shape[1]
+
+    def mirror_kv_append(self, kv: KV, rows: Rows, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                         rope: Optional[Rope] = None, q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+        """k, v [L, R, Hkv, d] into the cache's pages (keys turned to their positions), q [L, R, Hq, d] turned into q_out; the three may
+        be columns of one tensor.  Returns q_out."""
+        Hq, Hkv, d = self.desc.n_q_heads, self.desc.n_kv_heads, self.desc.head_dim
+        kp, kv_row, kv_layer = self._strided(k, Hkv, rows, "k")
+        vp, v_row, v_layer = self._strided(v, Hkv, rows, "v")
+        if (v_row, v_layer) != (kv_row, kv_layer):
+            raise ValueError("k and v must have the same strides")
+        if k.shape[0] != kv.num_layers or v.shape[0] != kv.num_layers:
+            raise ValueError("k and v must have the cache's layers")
+        qp, q_row, q_layer = None, 0, 0
+        if q is not None:
+            qp, q_row, q_layer = self._strided(q, Hq, rows, "q")
+            if q_out is None:
+                q_out = torch.empty((kv.num_layers, rows.n_rows, Hq, d), dtype=torch.bfloat16, device=self.device)
+            if q.shape[0] != kv.num_layers or q_out.shape != q.shape:
+                raise ValueError("q and q_out must be [L, R, Hq, d] with the cache's layers")
+        _check(self.lib.mirror_kv_append(self._ctx, C.byref(kv), C.byref(rows), C.byref(rope) if rope is not None else None, qp, q_row, q_layer,
+                                         _ptr(q_out, torch.bfloat16, "q_out") if q is not None else None, kp, vp, kv_row, kv_layer,
+                                         _stream(stream)), "mirror_kv_append")
+        return q_out
+
+    def mirror_attn_causal(self, kv: KV, rows: Rows, q: torch.Tensor, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
+                           lse_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Causal attention of the rows [L, R, Hq, d] over the cache (their own keys and values appended before); window tokens and the
+        first `sinks` are visible (window 0: all).  lse_out: fp32 [L, R, Hq]."""
+        shape = (kv.num_layers, rows.n_rows, self.desc.n_q_heads, self.desc.head_dim)
+        if out is None:
+            out = torch.empty_like(q)
+        if tuple(q.shape) != shape or tuple(out.shape) != shape or (lse_out is not None and tuple(lse_out.shape) != shape[:3]):
+            raise ValueError(f"q and out must be {shape}, lse_out {shape[:3]}")
+        key = ("rows", rows.batch, rows.n_rows)
+        need = self._need.get(key)
+        if need is None:
+            n = C.c_size_t()
+            _check(self.lib.mirror_rows_workspace_bytes(self._ctx, C.byref(rows), C.byref(n)), "mirror_rows_workspace_bytes")
+            need = n.value
+            if len(self._need) < 4096:
+                self._need[key] = need
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            _check(self.lib.mirror_set_workspace(self._ctx, C.c_void_p(self._ws.data_ptr()), need), "mirror_set_workspace")
+        _check(self.lib.mirror_attn_causal(self._ctx, C.byref(kv), C.byref(rows), window, sinks, _ptr(q, torch.bfloat16, "q"),
+                                           _ptr(out, torch.bfloat16, "out"), _ptr(lse_out, torch.float32, "lse_out"), _stream(stream)),
+               "mirror_attn_causal")
+        return out
+
+    def mirror_sample(self, logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                      top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                      want_probs: bool = False, want_logits: bool = False, stream=None) -> dict:
+        """One token of each row of logits fp32 [M, V] (rows may be strided) from uniforms u [M], under per-row filters (tensors [M], None: off).
+        probs: the filtered distribution, q_probs of accept_in; logits: what mirror_accept_select takes as a target's, with an lse of zeros."""
+        M, V = logits.shape
+        if V != self.desc.vocab:
+            raise ValueError(f"logits must have {self.desc.vocab} columns, got {V}")
+        if not logits.is_cuda or logits.dtype is not torch.float32 or (V > 1 and logits.stride(1) != 1):
+            raise ValueError("logits must be a CUDA tensor of torch.float32 with contiguous rows")
+        for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+            if t is not None and t.numel() != M:
+                raise ValueError(f"{name} must have {M} entries")
+        dev = logits.device
+        res = dict(token=torch.empty(M, dtype=torch.int32, device=dev), n_kept=torch.empty(M, dtype=torch.int32, device=dev),
+                   logprob=torch.empty(M, dtype=torch.float32, device=dev),
+                   probs=torch.empty((M, V), dtype=torch.float32, device=dev) if want_probs else None,
+                   logits=torch.empty((M, V), dtype=torch.float32, device=dev) if want_logits else None)
+        _check(self.lib.mirror_sample(self._ctx, logits.data_ptr(), logits.stride(0) if M > 1 else V, M,
+                                      _ptr(temperature, torch.float32, "temperature"), _ptr(top_k, torch.int32, "top_k"),
+                                      _ptr(top_p, torch.float32, "top_p"), _ptr(min_p, torch.float32, "min_p"), _ptr(u, torch.float32, "u"),
+                                      _ptr(res["token"]), _ptr(res["logprob"]), _ptr(res["n_kept"]), _ptr(res["probs"]),
+                                      _ptr(res["logits"]), _stream(stream)), "mirror_sample")
+        return res
 
     # ---- the target's layers around the attention ---------------------------------------------
     def target(self, layers: Sequence[dict], norm_final: torch.Tensor, intermediate: int, rope_theta: float = 1e6,

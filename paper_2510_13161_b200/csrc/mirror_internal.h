@@ -67,6 +67,8 @@ struct mirror_ctx {
     PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
 };
 
+mirror_status mirror_check_kv(const mirror_ctx* ctx, const mirror_kv* kv);          // what every call that reads the cache wants of it
+mirror_status mirror_check_rows(const mirror_rows* rows);
 mirror_status mirror_build_tree(const mirror_tree* tree, MirrorTreeInfo* info);
 
 // Workspace carving.  The layout depends only on the model shape and the row count M, so every entry

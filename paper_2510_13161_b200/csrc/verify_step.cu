@@ -4,18 +4,17 @@
 
 #include "mirror_internal.h"
 
-namespace {
-
-mirror_status check_kv(const mirror_ctx* ctx, const mirror_kv* kv, const mirror_tree* tree) {
+mirror_status mirror_check_kv(const mirror_ctx* ctx, const mirror_kv* kv) {
     if (!kv->k_pool || !kv->v_pool || !kv->page_table || !kv->prefix_len) return MIRROR_ERR_ARG;
     if (kv->num_layers <= 0 || kv->num_pages <= 0 || kv->max_pages_per_req <= 0) return MIRROR_ERR_ARG;
     if (((uintptr_t)kv->k_pool & 15) || ((uintptr_t)kv->v_pool & 15)) return MIRROR_ERR_ARG;
     const int64_t page_elems = (int64_t)ctx->desc.n_kv_heads * ctx->desc.page_size * ctx->desc.head_dim;
     if (kv->num_layers > 1 && (kv->layer_stride < (int64_t)kv->num_pages * page_elems)) return MIRROR_ERR_SHAPE;
     if (kv->layer_stride % page_elems != 0) return MIRROR_ERR_UNSUPPORTED;
-    (void)tree;
     return MIRROR_OK;
 }
+
+namespace {
 
 // Do two ranges of device memory have no byte in common?
 bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
@@ -28,7 +27,7 @@ extern "C" mirror_status mirror_attn_verify(mirror_ctx* ctx, const mirror_kv* kv
                                             const void* q, const void* k_new, const void* v_new, void* out,
                                             float* lse_out, void* stream) {
     if (!ctx || !kv || !tree || !q || !k_new || !v_new || !out) return MIRROR_ERR_ARG;
-    mirror_status st = check_kv(ctx, kv, tree);
+    mirror_status st = mirror_check_kv(ctx, kv);
     if (st != MIRROR_OK) return st;
     if (((uintptr_t)q & 15) || ((uintptr_t)k_new & 15) || ((uintptr_t)v_new & 15) || ((uintptr_t)out & 15)) return MIRROR_ERR_ARG;
     MirrorTreeInfo ti;
@@ -47,7 +46,7 @@ extern "C" mirror_status mirror_attn_verify_fp8(mirror_ctx* ctx, const mirror_kv
                                                 const float* v_scale, float q_scale, void* out, float* lse_out, void* stream) {
     if (!ctx || !kv || !tree || !q || !k_new_fp8 || !v_new_fp8 || !k_scale || !v_scale || !out || !(q_scale > 0.f)) return MIRROR_ERR_ARG;
     if (ctx->desc.head_dim != 128) return MIRROR_ERR_UNSUPPORTED;
-    mirror_status st = check_kv(ctx, kv, tree);
+    mirror_status st = mirror_check_kv(ctx, kv);
     if (st != MIRROR_OK) return st;
     if (((uintptr_t)q & 15) || ((uintptr_t)k_new_fp8 & 15) || ((uintptr_t)v_new_fp8 & 15) || ((uintptr_t)out & 15)) return MIRROR_ERR_ARG;
     MirrorTreeInfo ti;
@@ -126,7 +125,7 @@ mirror_status verify_step_impl(mirror_ctx* ctx, const mirror_kv* kv, const mirro
     if (!out->n_accepted || !out->best_branch || !out->n_emitted || !out->emitted || !out->accepted_nodes ||
         !out->decide_row || !out->reuse_slot)
         return MIRROR_ERR_ARG;
-    mirror_status st = check_kv(ctx, kv, tree);
+    mirror_status st = mirror_check_kv(ctx, kv);
     if (st != MIRROR_OK) return st;
     const bool spec = acc->mode == MIRROR_ACCEPT_SPEC_SAMPLING || acc->mode == MIRROR_ACCEPT_SPEC_TREE;
     if (!spec && acc->mode != MIRROR_ACCEPT_GREEDY) return MIRROR_ERR_ARG;

@@ -1,0 +1,127 @@
+"""mirror_attn_causal against the oracle in 64 bits; everything that no row sees is NaN in the cache."""
+import pytest
+import torch
+
+from paper_2510_13161_b200 import binding
+from tests.rows_helpers import PAGE, Case, check_attention, make
+
+pytestmark = pytest.mark.gpu
+
+LENS = [0, 1, 15, 16, 17, 31, 130, 500, 0, 999]
+
+
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (8, 2), (5, 1), (14, 2), (16, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_single_tokens(hq, hkv, d):
+    check_attention(make(hq, hkv, d), Case(hq, hkv, d, LENS, [1] * 10, layers=2, pad=2, seed=hq), False)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 0), (17, 16), (40, 3), (100, 33), (100, 200), (5000, 4)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_single_tokens_under_a_window(window, sinks, d):
+    check_attention(make(8, 2, d), Case(8, 2, d, LENS, [1] * 10, window=window, sinks=sinks, seed=window), False)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 2), (9, 5), (64, 17)])
+def test_a_few_rows(window, sinks):
+    counts = [2, 4, 0, 1, 3, 4, 4, 2, 0, 4]
+    check_attention(make(8, 2, 128), Case(8, 2, 128, LENS, counts, layers=2, pad=5, window=window, sinks=sinks, seed=4), False)
+    check_attention(make(2, 2, 64), Case(2, 2, 64, LENS, [c * 4 for c in counts], window=window, sinks=sinks, seed=5), False)
+
+
+def test_a_long_context_cut_over_all_ctas():
+    check_attention(make(8, 1, 128), Case(8, 1, 128, [20000], [1], seed=1), False)
+    check_attention(make(8, 2, 64), Case(8, 2, 64, [12345, 3, 0, 7000], [2, 1, 0, 2], seed=2, window=6000, sinks=40), False)
+
+
+def test_many_requests():
+    check_attention(make(2, 1, 64), Case(2, 1, 64, [(b * 13) % 90 for b in range(1024)], [b % 3 for b in range(1024)], seed=3), False)
+
+
+@pytest.mark.parametrize("spread", [8.0, 0.0])
+def test_scores_far_apart_and_all_alike(spread):
+    """Scores of +-100 and more: weights underflow, and the running maximum moves again and again."""
+    check_attention(make(8, 2, 128), Case(8, 2, 128, [700, 40], [1, 2], seed=6, spread=spread), False)
+
+
+def test_a_scale_of_its_own_and_uniform_rows():
+    check_attention(make(4, 2, 64, scale=0.3), Case(4, 2, 64, [33, 70, 5], [2, 2, 2], seed=7, uniform=True), False, scale=0.3)
+
+
+def test_twice_and_on_another_stream_the_same():
+    m = make(8, 2, 128)
+    c = Case(8, 2, 128, [3000, 77], [1, 1], seed=8)
+    a, la = check_attention(m, c, False)
+    s = torch.cuda.Stream()
+    out, lse = torch.empty_like(a), torch.empty_like(la)
+    q = c.q.cuda()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        m.mirror_attn_causal(c.kv, c.rows, q, out=out, lse_out=lse)
+    s.synchronize()
+    assert torch.equal(a, out) and torch.equal(la, lse)
+
+
+def test_captured_and_replayed_with_other_lengths():
+    """The partition is made on the device: a captured call follows the lengths that it finds."""
+    m = make(8, 2, 128)
+    c = Case(8, 2, 128, [1500, 900], [1, 1], seed=9)
+    kv, rows = c.device(m)
+    q, out = c.q.cuda(), torch.empty((1, 2, 8, 128), dtype=torch.bfloat16, device="cuda")
+    m.mirror_attn_causal(kv, rows, q, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        m.mirror_attn_causal(kv, rows, q, out=out)
+    lens = kv._refs[3]
+    for a, b in ((1500, 900), (3, 899), (0, 17)):
+        lens.copy_(torch.tensor([a, b], dtype=torch.int32))
+        g.replay()
+        got = out.clone()
+        m.mirror_attn_causal(kv, rows, q, out=out)
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and not out.isnan().any()
+    assert m.device_status() == (0, 0)
+
+
+def test_reports():
+    m = make(4, 2, 64)
+    c = Case(4, 2, 64, [20, 5], [1, 1], seed=1)
+    kv, rows = c.device(m)
+    q = c.q.cuda()
+    lens, table = kv._refs[3], kv._refs[2]
+    for name, change, code in (("length", lambda: lens.fill_(1000), 831), ("negative", lambda: lens.fill_(-1), 831), ("page", lambda: table.fill_(99), 832),
+                               ("page", lambda: table.fill_(-1), 832)):
+        kept = lens.clone(), table.clone()
+        table[table > 90] = 0
+        change()
+        m.mirror_attn_causal(kv, rows, q)
+        torch.cuda.synchronize()
+        assert m.device_status() == (6, code), name
+        lens.copy_(kept[0]), table.copy_(kept[1])
+    rows._refs[0].copy_(torch.tensor([0, 2, 1], dtype=torch.int32))          # a request with more rows than max_rows
+    table[table > 90] = 0
+    m.mirror_attn_causal(kv, rows, q)
+    torch.cuda.synchronize()
+    assert m.device_status() == (6, 830)
+
+
+def test_refusals():
+    m = make(4, 2, 64)
+    c = Case(4, 2, 64, [20, 5], [1, 1])
+    kv, rows = c.device(m)
+    q = c.q.cuda()
+    with pytest.raises(binding.MirrorError) as e:
+        m.mirror_attn_causal(kv, rows, q, window=-1)
+    assert e.value.code == 1
+    with pytest.raises(binding.MirrorError) as e:
+        m.mirror_attn_causal(kv, rows, q, sinks=-1)
+    assert e.value.code == 1
+    for bad in (q[:, :1], q.float(), q.transpose(1, 2)):
+        with pytest.raises(ValueError):
+            m.mirror_attn_causal(kv, rows, bad)
+    with pytest.raises(ValueError):
+        m.mirror_attn_causal(kv, rows, q, lse_out=torch.empty((1, 4, 2), device="cuda"))
+    m2 = make(4, 2, 64)
+    import ctypes as C
+    assert m2.lib.mirror_attn_causal(m2._ctx, C.byref(kv), C.byref(rows), 0, 0, q.data_ptr(), q.data_ptr(), None, None) == 4        # no workspace
