@@ -369,8 +369,9 @@ mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, const mirro
  *   lse_out   fp32 [L, R, Hq], nullable: natural-log softmax denominator
  * Pages that hold no visible token are not touched (their table entries may be anything), and what lies in a touched page beside
  * the tokens that some row of its request sees may be anything, infinities and NaN included.
- * Needs a workspace of mirror_rows_workspace_bytes().  Requests of few rows for now: max_rows * Hq / Hkv <= 16
- * (MIRROR_ERR_UNSUPPORTED otherwise). */
+ * Needs a workspace of mirror_rows_workspace_bytes().  Requests of few rows (max_rows * Hq / Hkv <= 16) stream the cache through
+ * warps; longer ones run on the tensor cores in tiles of 128 rows.  Rows whose positions lie beyond max_pages_per_req*16 are
+ * left as they are and reported through mirror_device_status, as are lengths below 0 and pages outside the pool. */
 mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, const mirror_rows* rows, size_t* bytes);
 mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mirror_rows* rows, int window, int n_sink,
                                  const void* q, void* out, float* lse_out, void* stream);

@@ -497,7 +497,7 @@ extern "C" mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, cons
     if (st != MIRROR_OK) return st;
     MirrorWsLayout L;
     mirror_ws_layout(ctx, 1, &L);
-    *bytes = L.end_attn;
+    *bytes = align_up(L.end_attn, 256) + mirror_attn_prompt_plan_bytes(ctx, rows);
     return MIRROR_OK;
 }
 
@@ -536,5 +536,5 @@ extern "C" mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv
     p.status = ctx->d_status;
     p.wait_limit = ctx->tune.wait_limit_cycles;
     if ((int64_t)p.max_rows * p.G <= kRows) return mirror_attn_token_launch(ctx, kv, p, (cudaStream_t)stream);
-    return MIRROR_ERR_UNSUPPORTED;
+    return mirror_attn_prompt_launch(ctx, kv, p, ws + align_up(L.end_attn, 256), (cudaStream_t)stream);
 }

@@ -70,13 +70,14 @@ __device__ __forceinline__ void load_request(const CausalParams& p, int b, int& 
         if (r0 < 0 || r1 > p.R || r1 - r0 > p.max_rows || r1 < r0) report(p.status, MIRROR_DEV_CHECK, 830);
         if (raw < 0 || (long long)raw + n > cap) report(p.status, MIRROR_DEV_CHECK, 831);
     }
+    n = min(n, cap - prefix);
 }
 __device__ __forceinline__ Request make_request(const CausalParams& p, int row0, int n, int prefix) {
     Request r;
     r.row0 = row0;
     r.n = n;
     r.prefix = prefix;
-    r.len = min(prefix + n, p.max_pages * kAttnSlotTok);
+    r.len = prefix + n;
     r.lo = p.window > 0 ? min(max(0, prefix - p.window + 1), r.len) : 0;
     r.sink = min(p.n_sink, r.lo);
     r.from = r.lo / kAttnSlotTok;

@@ -80,12 +80,11 @@ constexpr int kMergeSmem = kMergeSlots * 10 * 128 * 4;      // their columns, th
 // and the arithmetic runs out of shared memory (17 parts of 85 rows: 15 us with loads in the loop over the parts, 8 with
 // eight parts' loads in flight).
 // The caller has waited for the records, and lets the kernel behind be launched.
-// map(row, GroupBegin) -> false, or the row's node and query head; record(group, slot) -> its record in slot 0 (of the unit
+// map(row, GroupBegin) -> false, or the places of the row's output (in rows of D) and of its lse; record(group, slot) -> its record in slot 0 (of the unit
 // that began before the group's range) or 1, [column][128 rows], D accumulator columns, then (max, sum).  wait_limit: SM cycles
 // after which a wait gives up; stall: test aid, 1 makes the first wait run out (it expects bytes that nobody copies).
 template <int D, class Map, class Record>
-__device__ __forceinline__ void merge_boundary(const GroupBegin* table, int n_groups, int n, int Hq, int B, __nv_bfloat16* out, float* lse_out,
-                                               int* status, long long wait_limit, int stall, Map map, Record record) {
+__device__ __forceinline__ void merge_boundary(const GroupBegin* table, int n_groups, __nv_bfloat16* out, float* lse_out, int* status, long long wait_limit, int stall, Map map, Record record) {
     extern __shared__ __align__(128) float s_cols[];                            // [slot][8 columns][128 rows]
     float(*const s_ml)[2][128] = (float(*)[2][128])(s_cols + kMergeSlots * 8 * 128);     // [part][max, then weight | sum][128 rows]
     __shared__ GroupBegin s_begin[512];
@@ -105,9 +104,8 @@ __device__ __forceinline__ void merge_boundary(const GroupBegin* table, int n_gr
     const int n_blocks = parts - 1, j_blk = g - (ga + 1);
     constexpr int kChunks = D / 8;                                              // 8 output columns, 2 of them a thread quarter's
     const int row = tid & 127, cq = tid >> 7;
-    int node = 0, head = 0;
-    const bool has_row = map(row, u, node, head);
-    const size_t lb = (size_t)u.layer * B + u.b;
+    size_t place = 0, lse_place = 0;
+    const bool has_row = map(row, u, place, lse_place);
     // group ga holds the unit's first tile (its record is in slot 1), the later groups began inside the unit (slot 0)
     const float* const first = record(ga, 1);
     const float* const second = record(ga + 1, 0);
@@ -185,8 +183,8 @@ __device__ __forceinline__ void merge_boundary(const GroupBegin* table, int n_gr
             const int chunk = c0 + c * n_blocks;
             if (!has_row) continue;
             const float inv = 1.f / Lm;
-            *reinterpret_cast<uint32_t*>(out + ((lb * n + node) * (size_t)Hq + head) * D + chunk * 8 + cq * 2) = pack_bf16(a0 * inv, a1 * inv);
-            if (lse_out && chunk == 0 && cq == 0) lse_out[(lb * Hq + head) * n + node] = Mm * kAttnLn2 + logf(Lm);
+            *reinterpret_cast<uint32_t*>(out + place * D + chunk * 8 + cq * 2) = pack_bf16(a0 * inv, a1 * inv);
+            if (lse_out && chunk == 0 && cq == 0) lse_out[lse_place] = Mm * kAttnLn2 + logf(Lm);
         }
     }
 }

@@ -1,0 +1,789 @@
+// Causal attention of prompts (mirror_attn_causal with more than 16 rows per KV head), on the tensor cores.
+//
+// Rows that share one KV head's stream, the gs query heads of the group times tokens, are cut in tiles of at most 128 rows (whole tokens).  A
+// unit is (layer, KV head, two neighbouring row tiles of one request); a CTA works on both tiles as two streams over the same K/V tiles in
+// shared memory, since one stream alone is a chain (Q K^T -> softmax -> P V) that leaves the tensor cores idle for as long as its
+// softmax takes.  A unit's keys are the 16-token slots that some row of it sees: the first slots that stay visible (sinks), then from
+// the window of its first row to its last row; eight slots to a tile of 128 keys.  What no row of a stream sees of a tile is neither
+// multiplied nor exponentiated.
+//
+// The tiles of all units form one sequence that is split evenly over the CTAs, one per SM: prompts are causal, so units are of any
+// length, and a few short requests behind a long prefix are few units.  attn_prompt_plan_kernel counts the tiles (they depend on lengths
+// that only the device knows) and finds where each CTA begins; a unit that a boundary cuts leaves a (max, sum, accumulator) record per
+// part and stream, which attn_prompt_merge_kernel combines in the order of the parts.
+//
+// Per CTA, 12 warps (as in attn_verify.cu, whose softmax this shares; see there for the offset that stands in for a running maximum):
+//   warps 0, 3   stage K and V tiles into one ring; the V warp stages Q too
+//   warps 1, 2   issue, one stream each and in turns, P V of one tile and Q K^T of the next.  Warp 1 owns tensor memory
+//   warps 4..7, 8..11  softmax of stream 0 and of stream 1, a thread per row
+// TMEM: S0 | S1 (128 columns each) | O0 | O1 (d columns each).
+// Every mbarrier wait is bounded; on expiry the kernel records MIRROR_DEV_TIMEOUT and unwinds.
+#include <math.h>
+
+#include <algorithm>
+
+#include "attn_causal.h"
+#include "attn_softmax.h"
+
+namespace {
+
+using namespace attn;
+
+constexpr int kThreads = 384;
+constexpr int kSlotTok = kAttnSlotTok;
+constexpr int kTileSlots = 8;
+constexpr int kTileTok = kSlotTok * kTileSlots;     // 128
+constexpr int kRows = 128;                          // UMMA M: rows of a stream
+constexpr int kMaxStages = 10;
+constexpr int kTmemCols = 512;
+constexpr int kTmemO = 2 * kTileTok;
+constexpr int kCtrlBytes = 512;
+constexpr size_t kSmemLimit = 232448;               // 227 KB
+constexpr int kPlanThreads = 1024;
+constexpr int kSnapTiles = 2;                       // a boundary moves to a unit boundary that is at most this many tiles away
+
+// One pair of row tiles of one request, the same for all layers and heads.
+struct PairClass {
+    int row0, n, prefix;                  // the request's rows
+    int tok;                              // the pair's first token
+    int tiles, cum;                       // K/V tiles; tiles of the classes before it
+    int b, pad;
+};
+// Where a CTA begins, and how many tiles it has.
+struct CtaStart {
+    int layer, hs, cls, t;
+    int n_tiles;
+    int pad[3];
+};
+static_assert(sizeof(PairClass) == 32 && sizeof(CtaStart) == 32, "two 16-byte loads each");
+
+struct PromptParams {
+    CausalParams c;
+    int gs, shares;                       // query heads of a row tile; shares of a group's heads (1 unless G > 128)
+    int nt;                               // tokens of a row tile
+    int n_hs;                             // KV heads x shares
+    int n_cta;
+    int max_classes;
+    PairClass* classes;
+    CtaStart* starts;                     // [n_cta + 1] (the last one's cls: how many classes there are)
+};
+
+struct Maps {
+    CUtensorMap k, v, q;
+};
+
+// The keys of a pair: [0, sink) and [lo, end), in slots as in causal::Request.
+struct Keys {
+    int lo, sink, end, sink_slots, from, slots;
+    __device__ __forceinline__ int page(int t) const { return t < sink_slots ? t : t - sink_slots + from; }
+};
+__device__ __forceinline__ Keys pair_keys(const PromptParams& p, int n, int prefix, int tok) {
+    Keys k;
+    k.end = prefix + min(tok + 2 * p.nt, n);
+    k.lo = p.c.window > 0 ? min(max(0, prefix + tok - p.c.window + 1), k.end) : 0;
+    k.sink = min(p.c.n_sink, k.lo);
+    k.from = k.lo / kSlotTok;
+    k.sink_slots = min((k.sink + kSlotTok - 1) / kSlotTok, k.from);
+    k.slots = k.sink_slots + (k.end + kSlotTok - 1) / kSlotTok - k.from;
+    return k;
+}
+
+// ---- the plan: one block ---------------------------------------------------------------------------------------
+__device__ int block_scan(int v, int* s_warp, int* total) {              // inclusive, over the block
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = v;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 32; ++w) {
+        if (w < warp) before += s_warp[w];
+        all += s_warp[w];
+    }
+    *total = all;
+    return v + before;
+}
+__global__ void __launch_bounds__(kPlanThreads) attn_prompt_plan_kernel(const __grid_constant__ PromptParams p) {
+    __shared__ int s_base[kAttnMaxBatch + 1], s_row0[kAttnMaxBatch], s_n[kAttnMaxBatch], s_prefix[kAttnMaxBatch], s_warp[kPlanThreads / 32];
+    __shared__ int s_at[kPlanThreads];                   // where the CTAs begin in the sequence
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    const int tid = threadIdx.x;
+    int n_cls = 0;
+    {
+        int pairs = 0;
+        if (tid < p.c.B) {
+            int row0, n, prefix;
+            causal::load_request(p.c, tid, row0, n, prefix, true);
+            s_row0[tid] = row0; s_n[tid] = n; s_prefix[tid] = prefix;
+            pairs = (n + 2 * p.nt - 1) / (2 * p.nt);
+        }
+        const int incl = block_scan(pairs, s_warp, &n_cls);
+        if (tid < p.c.B) s_base[tid + 1] = incl;
+        if (tid == 0) s_base[0] = 0;
+    }
+    __syncthreads();
+    if (n_cls > p.max_classes) {                         // (overlapping requests: more rows than there are)
+        if (tid == 0) causal::report(p.c.status, MIRROR_DEV_CHECK, 830);
+        n_cls = 0;
+    }
+    int total = 0;
+    for (int c0 = 0; c0 < n_cls; c0 += kPlanThreads) {
+        const int c = c0 + tid;
+        PairClass u = {};
+        if (c < n_cls) {
+            int lo = 0, hi = p.c.B - 1;                  // the first b with s_base[b + 1] > c
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (s_base[mid + 1] > c) hi = mid; else lo = mid + 1;
+            }
+            u.b = lo;
+            u.row0 = s_row0[lo]; u.n = s_n[lo]; u.prefix = s_prefix[lo];
+            u.tok = (c - s_base[lo]) * 2 * p.nt;
+            u.tiles = max((pair_keys(p, u.n, u.prefix, u.tok).slots + kTileSlots - 1) / kTileSlots, 1);
+        }
+        int all;
+        const int incl = block_scan(u.tiles, s_warp, &all);
+        u.cum = total + incl - u.tiles;
+        if (c < n_cls) p.classes[c] = u;
+        total += all;
+    }
+    // (every thread has the same total)
+    const long long seq = (long long)p.c.L * p.n_hs * total;
+    if (seq >= (1ll << 31)) {
+        if (tid == 0) causal::report(p.c.status, MIRROR_DEV_CHECK, 833);
+        n_cls = total = 0;
+    }
+    __syncthreads();                                     // classes[] written by this block are read below
+    if (tid <= p.n_cta) {
+        // boundary tid of n_cta + 1
+        const int used = (int)min((long long)p.n_cta, max(seq, 1ll));
+        CtaStart s = {};
+        long long x = 0;
+        if (total == 0 || tid >= used) {
+            x = total == 0 ? 0 : seq;
+        } else if (tid > 0) {
+            x = seq * tid / used;
+            const long long share = seq / used;
+            const int per = total;                       // tiles of one (layer, head)
+            const long long lh = x / per;
+            int rem = (int)(x - lh * per);
+            int lo = 0, hi = n_cls - 1;                  // the last class with cum <= rem
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (p.classes[mid].cum <= rem) lo = mid; else hi = mid - 1;
+            }
+            const PairClass u = p.classes[lo];
+            s.layer = (int)(lh / p.n_hs);
+            s.hs = (int)(lh - (long long)s.layer * p.n_hs);
+            s.cls = lo;
+            s.t = rem - u.cum;
+            const int tol = (int)min((long long)kSnapTiles, share >> 2);
+            if (s.t <= tol) {
+                x -= s.t;
+                s.t = 0;
+            } else if (u.tiles - s.t <= tol) {
+                x += u.tiles - s.t;
+                s.t = 0;
+                if (++s.cls == n_cls) {
+                    s.cls = 0;
+                    if (++s.hs == p.n_hs) { s.hs = 0; ++s.layer; }
+                }
+            }
+        }
+        s_at[tid] = (int)x;
+        if (tid < p.n_cta) {
+            p.starts[tid] = s;
+            p.c.begins[tid] = {x < seq && s.t > 0 ? 1 : 0, s.layer, s.cls, s.hs};
+        }
+    }
+    __syncthreads();
+    if (tid < p.n_cta) p.starts[tid].n_tiles = s_at[tid + 1] - s_at[tid];
+    if (tid == 0) p.starts[p.n_cta].cls = n_cls;
+}
+
+// ---- a CTA's way through its units -----------------------------------------------------------------------------
+struct Segment {
+    int layer, hs, cls;
+    int t_first, t_last, tiles;           // tiles [t_first, t_last) of the unit's `tiles`
+    PairClass u;
+    Keys k;
+};
+__device__ __forceinline__ PairClass load_class(const PromptParams& p, int cls) {
+    const int4* src = reinterpret_cast<const int4*>(p.classes + cls);
+    const int4 a = src[0], b = src[1];
+    PairClass u;
+    u.row0 = a.x; u.n = a.y; u.prefix = a.z; u.tok = a.w;
+    u.tiles = b.x; u.cum = b.y; u.b = b.z; u.pad = 0;
+    return u;
+}
+__device__ __forceinline__ void fill_segment(Segment& s, const PromptParams& p, int left) {
+    s.tiles = s.u.tiles;
+    s.t_last = min(s.tiles, s.t_first + left);
+    s.k = pair_keys(p, s.u.n, s.u.prefix, s.u.tok);
+}
+__device__ __noinline__ void next_segment(Segment& s, const PromptParams& p, int n_cls, int left) {
+    if (++s.cls == n_cls) {
+        s.cls = 0;
+        if (++s.hs == p.n_hs) { s.hs = 0; ++s.layer; }
+    }
+    s.u = load_class(p, s.cls);
+    s.t_first = 0;
+    fill_segment(s, p, left);
+}
+// Does some row of stream g see something of tile t?  (Its tokens are tok + g nt and the nt - 1 behind it, as far as they exist.)
+struct StreamRows {
+    int first, last;                      // positions; last < first: no rows
+};
+__device__ __forceinline__ StreamRows stream_rows(const PromptParams& p, const Segment& s, int g) {
+    const int t0 = s.u.tok + g * p.nt, t1 = min(t0 + p.nt, s.u.n) - 1;
+    return {s.u.prefix + t0, s.u.prefix + t1};
+}
+__device__ __forceinline__ bool tile_seen(const PromptParams& p, const Segment& s, const StreamRows& r, int t) {
+    const int key0 = s.k.page(t * kTileSlots) * kSlotTok, key1 = s.k.page(min(t * kTileSlots + kTileSlots, s.k.slots) - 1) * kSlotTok + kSlotTok - 1;
+    return r.last >= r.first && key0 <= r.last && (p.c.window == 0 || key1 > r.first - p.c.window || key0 < p.c.n_sink);
+}
+
+struct Ctrl {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t q_full, q_empty;
+    uint64_t s_full[2], p_full[2][2], o_full[2];        // per stream (P: per half of the tile)
+    uint64_t pv_half[2];
+    uint64_t turn[2];                                   // the issuing warps take turns
+    uint64_t exp_turn[2][4];                            // the two softmax warps of a scheduler take turns
+    CtaStart start;
+    int n_cls;
+    int* status;
+    long long wait_limit;
+    uint32_t tmem_base;
+    volatile int abort;
+};
+static_assert(sizeof(Ctrl) <= kCtrlBytes, "control block");
+
+template <int D>
+struct Cfg {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kSlotBytes = kHalves * kSlotTok * 128;
+    static constexpr int kGroupStride = kHalves * 1024;
+    static constexpr int kStageBytes = kTileSlots * kSlotBytes;
+    static constexpr int kQHalfBytes = kRows * 128;
+    static constexpr int kQBytes = kHalves * kQHalfBytes;
+};
+
+// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM.
+__device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, const Keys& k, int pos, int window, int n_sink) {
+#pragma unroll 1
+    for (int c = 0; c < kTileSlots; ++c) {
+        uint32_t m = 0;
+        if (slot0 + c < k.slots) {
+            const int key0 = k.page(slot0 + c) * kSlotTok, at = pos - key0;             // the row's own token, in the slot
+            m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
+            if (window > 0) {
+                const int lo = at - window + 1, sk = n_sink - key0;
+                const uint32_t in = lo <= 0 ? 0xffffu : lo > 15 ? 0u : 0xffffu & ~((1u << lo) - 1u);
+                m &= in | (sk >= 16 ? 0xffffu : sk <= 0 ? 0u : (1u << sk) - 1u);
+            }
+        }
+        if (__all_sync(0xffffffffu, m == 0xffffu)) continue;
+        uint32_t r[16];
+        ptx::tmem_ld_32x32b_x16(s_addr + (uint32_t)(c * 16), r);
+        tmem_ld_wait16(r);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (!((m >> j) & 1u)) r[j] = 0xff800000u;
+        tmem_st_32x32b_x16(s_addr + (uint32_t)(c * 16), r);
+    }
+    tmem_st_wait();
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_constant__ Maps tm, const __grid_constant__ PromptParams p, const int n_stages) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* const sQ = smem;                                            // [2 streams]
+    uint8_t* const ring = sQ + 2 * C::kQBytes;                           // [n_stages] K or V tiles: K of a tile, V of it, K of the next
+    Ctrl* const ctrl = (Ctrl*)(ring + (size_t)n_stages * C::kStageBytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // ---- prologue, while the kernel ahead is still running: nothing of global memory is touched
+    if (tid == 0) {
+        for (int s = 0; s < n_stages; ++s) { ptx::mbar_init(&ctrl->full[s], 1); ptx::mbar_init(&ctrl->empty[s], 2); }
+        ptx::mbar_init(&ctrl->q_full, 1);
+        ptx::mbar_init(&ctrl->q_empty, 2);
+        for (int g = 0; g < 2; ++g) {
+            ptx::mbar_init(&ctrl->s_full[g], 1); ptx::mbar_init(&ctrl->p_full[g][0], 4); ptx::mbar_init(&ctrl->p_full[g][1], 4);
+            ptx::mbar_init(&ctrl->o_full[g], 1); ptx::mbar_init(&ctrl->turn[g], 1); ptx::mbar_init(&ctrl->pv_half[g], 1);
+            for (int s = 0; s < 4; ++s) ptx::mbar_init(&ctrl->exp_turn[g][s], 1);
+        }
+        ctrl->abort = 0;
+        ctrl->status = p.c.status;
+        ctrl->wait_limit = p.c.wait_limit;
+        ptx::fence_mbar_init();
+        ptx::prefetch_tmap(&tm.k); ptx::prefetch_tmap(&tm.v); ptx::prefetch_tmap(&tm.q);
+    }
+    // rows that the Q copies do not fill are zeros
+    const int q_rows = p.gs * p.nt, pad = kRows - q_rows;
+    for (int i = tid; i < 2 * C::kHalves * pad * 8; i += kThreads) {
+        const int half = i / (pad * 8), c = i - half * pad * 8;
+        *reinterpret_cast<uint4*>(sQ + half * C::kQHalfBytes + q_rows * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+    }
+    ptx::fence_proxy_async();
+    if (warp == 1) {
+        ptx::tmem_alloc(&ctrl->tmem_base, kTmemCols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    if (tid == 0) {
+        ctrl->start = p.starts[blockIdx.x];
+        ctrl->n_cls = p.starts[p.n_cta].cls;                           // (left there by the plan)
+    }
+    __syncthreads();
+    const uint32_t tmem_base = ctrl->tmem_base;
+    const int n_tiles = ctrl->start.n_tiles, n_cls = ctrl->n_cls;
+    auto first_segment = [&](Segment& s) {
+        s.layer = ctrl->start.layer; s.hs = ctrl->start.hs; s.cls = ctrl->start.cls; s.t_first = ctrl->start.t;
+        s.u = load_class(p, s.cls);
+        fill_segment(s, p, n_tiles);
+    };
+
+    if (n_tiles <= 0) {
+        // (no tiles: nothing to do)
+    } else if (warp == 0 || warp == 3) {
+        // ======================================================================= K and V producers, Q with V
+        const bool V = warp == 3;
+        const CUtensorMap* const map = V ? &tm.v : &tm.k;
+        Segment sg;
+        first_segment(sg);
+        int left = n_tiles, t = sg.t_first;
+        uint32_t seq = V ? 1 : 0, n_seg = 0;
+        bool ok = true;
+        int pg = 0, pg_next = 0;
+        auto fetch = [&](int tt) -> int {                            // physical pages of a tile, one per lane (0..7)
+            const int sl = tt * kTileSlots + lane;
+            return (lane < kTileSlots && sl < sg.k.slots) ? p.c.page_table[(size_t)sg.u.b * p.c.max_pages + sg.k.page(sl)] : 0;
+        };
+        auto load_q = [&]() {
+            if (!ptx::warp_wait(ctrl, &ctrl->q_empty, (n_seg & 1) ^ 1, 61)) { ok = false; return; }
+            if (ptx::elect_one()) {
+                const int kvh = sg.hs / p.shares, head = kvh * p.c.G + (sg.hs - kvh * p.shares) * p.gs;
+                ptx::mbar_arrive_expect_tx(&ctrl->q_full, (uint32_t)(2 * C::kHalves * q_rows * 128));
+                for (int g = 0; g < 2; ++g)
+                    for (int h = 0; h < C::kHalves; ++h)
+                        ptx::tma_load_5d(sQ + g * C::kQBytes + h * C::kQHalfBytes, &tm.q, &ctrl->q_full, 0, head, sg.layer * p.c.R + sg.u.row0 + sg.u.tok + g * p.nt, h, 0);
+            }
+            __syncwarp();
+            ++n_seg;
+        };
+        // what some row of the request sees (see causal::Request); the rest of V may be anything, and is taken as zeros
+        int req_lo = 0, req_sink = 0, req_len = 0;
+        auto request = [&]() {
+            req_len = sg.u.prefix + sg.u.n;
+            req_lo = p.c.window > 0 ? min(max(0, sg.u.prefix - p.c.window + 1), req_len) : 0;
+            req_sink = min(p.c.n_sink, req_lo);
+        };
+        request();
+        pg_next = fetch(t);
+        if (V) load_q();
+#pragma unroll 1
+        while (left > 0 && ok) {
+            pg = pg_next;
+            if (t + 1 < sg.t_last) pg_next = fetch(t + 1);
+            const uint32_t st = seq % (uint32_t)n_stages;
+            if (!ptx::warp_wait(ctrl, &ctrl->empty[st], ((seq / (uint32_t)n_stages) & 1) ^ 1, 60)) { ok = false; break; }
+            uint8_t* const dst = ring + (size_t)st * C::kStageBytes;
+            uint64_t* const bar = &ctrl->full[st];
+            const int sl0 = t * kTileSlots, n_sl = min(kTileSlots, sg.k.slots - sl0), kvh = sg.hs / p.shares;
+            if (pg < 0 || pg >= p.c.num_pages) { causal::report(p.c.status, MIRROR_DEV_CHECK, 832); pg = 0; }
+            const int row0 = sg.layer * p.c.layer_pages;
+            uint32_t partial = 0;                                    // V: slots with tokens that no row of the request sees
+            if (V) {
+                const int key0 = sg.k.page(sl0 + (lane & 7)) * kSlotTok;
+                partial = __ballot_sync(0xffffffffu, lane < n_sl && (key0 + kSlotTok > req_len || (key0 < req_lo && key0 + kSlotTok > req_sink)));
+                if (partial) {
+                    for (int k = 0; k < n_sl; ++k) {
+                        if (!(partial >> k & 1)) continue;
+                        const int page = __shfl_sync(0xffffffffu, pg, k), base = sg.k.page(sl0 + k) * kSlotTok;
+                        const uint8_t* const src = (const uint8_t*)p.c.v_pool + ((size_t)(row0 + page) * p.c.Hkv + kvh) * (size_t)C::kSlotBytes;
+                        constexpr int kRowChunks = D / 8;
+#pragma unroll 1
+                        for (int c = lane; c < kSlotTok * kRowChunks; c += 32) {
+                            const int tr = c / kRowChunks, cc = c % kRowChunks, key = base + tr;
+                            const bool seen = key < req_len && (key >= req_lo || key < req_sink);
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                                         ::"r"(ptx::smem_u32(dst + k * C::kSlotBytes + kv_slot_off<C::kHalves>(tr, cc))), "l"(src + c * 16), "r"(seen ? 16u : 0u) : "memory");
+                        }
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    ptx::fence_proxy_async();
+                    __syncwarp();
+                }
+            }
+            // (the barrier's one arrival is its arming, so copies that land before it cannot complete the phase)
+            if (n_sl == kTileSlots && !partial) {
+                int row[kTileSlots];
+#pragma unroll
+                for (int k = 0; k < kTileSlots; ++k) row[k] = (row0 + __shfl_sync(0xffffffffu, pg, k)) * p.c.Hkv + kvh;
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(bar, (uint32_t)C::kStageBytes);
+#pragma unroll
+                    for (int k = 0; k < kTileSlots; ++k) ptx::tma_load_5d(dst + k * C::kSlotBytes, map, bar, 0, 0, 0, 0, row[k]);
+                }
+            } else {
+                const bool leader = ptx::elect_one();
+                if (leader) ptx::mbar_arrive_expect_tx(bar, (uint32_t)((n_sl - __popc(partial)) * C::kSlotBytes));
+#pragma unroll 1
+                for (int k = 0; k < n_sl; ++k) {
+                    const int page = __shfl_sync(0xffffffffu, pg, k);
+                    if (leader && !(partial >> k & 1)) ptx::tma_load_5d(dst + k * C::kSlotBytes, map, bar, 0, 0, 0, 0, (row0 + page) * p.c.Hkv + kvh);
+                }
+            }
+            __syncwarp();
+            seq += 2;
+            --left;
+            if (++t == sg.t_last && left > 0) {
+                next_segment(sg, p, n_cls, left);
+                t = 0;
+                request();
+                pg_next = fetch(0);
+                if (V) load_q();
+            }
+        }
+        if (!ok) {
+            // let copies already on the way land before the CTA's shared memory goes away
+            for (int k = 0; k <= n_stages / 2 + 1 && seq >= 2; ++k) {
+                seq -= 2;
+                ptx::mbar_wait(&ctrl->full[seq % (uint32_t)n_stages], (seq / (uint32_t)n_stages) & 1, 20000000ll);
+            }
+            if (V && n_seg > 0) ptx::mbar_wait(&ctrl->q_full, (n_seg - 1) & 1, 20000000ll);
+        }
+    } else if (warp < 4) {
+        // ======================================================================= tensor-core issuers (see attn_verify.cu)
+        const uint32_t hi_q = ptx::umma_desc_hi_sw128(1024), hi_k = ptx::umma_desc_hi_sw128(C::kGroupStride), hi_v = hi_k;
+        const int g = warp - 1;
+        const uint32_t q_lo = ptx::umma_desc_lo(ptx::smem_u32(sQ + g * C::kQBytes), 16);
+        const uint32_t k_lo = ptx::umma_desc_lo(ptx::smem_u32(ring), 16);
+        const uint32_t v_lo = ptx::umma_desc_lo(ptx::smem_u32(ring), 1024);        // MN-major: LBO = next 64-column atom
+        const uint32_t idesc_pv = ptx::umma_idesc_bf16(kRows, D) | (1u << 16);
+        const uint32_t q_half = (uint32_t)(C::kQHalfBytes >> 4);
+        const uint32_t s_d = tmem_base + (uint32_t)(g * kTileTok), o_d = tmem_base + kTmemO + (uint32_t)(g * D);
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, uint32_t parity, int where) { ok = ok && ptx::warp_wait(ctrl, bar, parity, where); };
+        uint32_t st = 0, ph = 0;
+        auto take = [&]() -> uint32_t {
+            const uint32_t s = st;
+            wait(&ctrl->full[s], ph, 62);
+            if (++st == (uint32_t)n_stages) { st = 0; ph ^= 1; }
+            return s;
+        };
+        uint32_t p_par = 0, q_par = 0, turn_par = g == 0 ? 1 : 0;
+        Segment sg;
+        first_segment(sg);
+        StreamRows rows = stream_rows(p, sg, g);
+        int left = n_tiles, t = sg.t_first;                          // the tile whose Q K^T comes next
+        bool has_pv = false, pv_on = false, pv_last = false, started = false;
+        int pv_sl = 0;
+#pragma unroll 1
+        while (ok) {
+            const bool has_qk = left > 0;
+            uint32_t vst = 0, kst = 0;
+            if (has_pv) vst = take();
+            if (has_qk) {
+                kst = take();
+                if (t == sg.t_first) { wait(&ctrl->q_full, q_par, 63); q_par ^= 1; }
+            }
+            const uint32_t vb = v_lo + vst * (uint32_t)(C::kStageBytes >> 4);
+            auto pv = [&](int k0, int k1) {
+#pragma unroll 1
+                for (int k = k0; k < k1; ++k)
+                    ptx::umma_f16_tmem_a(o_d, s_d + (uint32_t)(k * 8), vb + (uint32_t)(k * (C::kSlotBytes / 16)), hi_v, idesc_pv, k > 0 || started);
+            };
+            if (has_pv) {
+                wait(&ctrl->p_full[g][0], p_par, 64);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                if (ptx::elect_one()) {
+                    if (pv_on) pv(0, min(pv_sl, kTileSlots / 2));
+                    ptx::umma_commit(&ctrl->pv_half[g]);
+                }
+                __syncwarp();
+                wait(&ctrl->p_full[g][1], p_par, 65);
+                p_par ^= 1;
+            }
+            wait(&ctrl->turn[g], turn_par, 66);
+            turn_par ^= 1;
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const bool qk_on = has_qk && tile_seen(p, sg, rows, t), qk_last = has_qk && t + 1 == sg.t_last;
+            const int qk_sl = has_qk ? min(kTileSlots, sg.k.slots - t * kTileSlots) : 0;
+            const uint32_t idesc_qk = ptx::umma_idesc_bf16(kRows, qk_sl * kSlotTok), kb = k_lo + kst * (uint32_t)(C::kStageBytes >> 4);
+            if (ptx::elect_one()) {
+                if (has_pv) {
+                    if (pv_on) pv(kTileSlots / 2, pv_sl);
+                    ptx::umma_commit(&ctrl->empty[vst]);
+                    if (pv_last) ptx::umma_commit(&ctrl->o_full[g]);
+                }
+                if (has_qk) {
+                    if (qk_on) {
+#pragma unroll 1
+                        for (int kk = 0; kk < D / 16; ++kk)
+                            ptx::umma_f16_lohi(s_d, q_lo + (kk >> 2) * q_half + (uint32_t)((kk & 3) * 2), hi_q, kb + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 2), hi_k, idesc_qk, kk != 0);
+                    }
+                    ptx::umma_commit(&ctrl->s_full[g]);
+                    ptx::umma_commit(&ctrl->empty[kst]);
+                    if (qk_last) ptx::umma_commit(&ctrl->q_empty);
+                }
+                ptx::mbar_arrive(&ctrl->turn[g ^ 1]);
+            }
+            __syncwarp();
+            if (!has_qk) break;
+            if (has_pv) started = pv_last ? false : started || pv_on;
+            has_pv = true;
+            pv_on = qk_on;
+            pv_last = qk_last;
+            pv_sl = qk_sl;
+            --left;
+            if (++t == sg.t_last && left > 0) {
+                next_segment(sg, p, n_cls, left);
+                rows = stream_rows(p, sg, g);
+                t = 0;
+            }
+        }
+    } else {
+        // ======================================================================= softmax
+        const int grp = (warp - 4) >> 2, w4 = warp & 3, row = w4 * 32 + lane;
+        const int it = row / p.gs, hl = row - it * p.gs;             // token of the tile, head of the share
+        const uint32_t lane_base = tmem_base + ((uint32_t)(w4 * 32) << 16);
+        const uint32_t s_addr = lane_base + (uint32_t)(grp * kTileTok), o_addr = lane_base + kTmemO + (uint32_t)(grp * D);
+        constexpr int kRowW = D + 4;                                 // record: D accumulator columns, then (max, sum)
+        const float sc = p.c.scale_log2e;
+        const uint64_t sc2 = pack2(sc, sc);
+        uint32_t t_par = grp == 0 ? 1 : 0, s_par = 0, o_par = 0;
+        auto take_turn = [&]() -> bool {
+            const bool r = ptx::warp_wait(ctrl, &ctrl->exp_turn[grp][w4], t_par, 67);
+            t_par ^= 1;
+            return r;
+        };
+        auto pass_turn = [&]() {
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&ctrl->exp_turn[grp ^ 1][w4]);
+        };
+        bool ok = true;
+        int left = n_tiles;
+        Segment sg;
+        first_segment(sg);
+#pragma unroll 1
+        while (left > 0 && ok) {
+            const StreamRows rows = stream_rows(p, sg, grp);
+            const int kvh = sg.hs / p.shares, hg = (sg.hs - kvh * p.shares) * p.gs + hl;                     // head within the group
+            const int tok = sg.u.tok + grp * p.nt + it, pos = sg.u.prefix + tok;
+            const bool row_ok = it < p.nt && tok < sg.u.n && hg < p.c.G;
+            const bool warp_has_rows = __any_sync(0xffffffffu, row_ok);
+            float off = row_ok ? -INFINITY : 1e30f, l_run = 0.f;
+            bool redone = false, any_tile = false;                   // any_tile: the accumulator holds something
+#pragma unroll 1
+            for (int t = sg.t_first; t < sg.t_last; ++t) {
+                const bool on = tile_seen(p, sg, rows, t);
+                if (!ptx::warp_wait(ctrl, &ctrl->s_full[grp], s_par, 68)) { ok = false; break; }
+                s_par ^= 1;
+                ptx::tc_fence_after();
+                if (warp_has_rows && on) {
+                    const int key0 = sg.k.page(t * kTileSlots) * kSlotTok;
+                    const bool whole_tile = (t + 1) * kTileSlots <= sg.k.slots && sg.k.page(t * kTileSlots + kTileSlots - 1) * kSlotTok + kSlotTok - 1 <= rows.first &&
+                                            (p.c.window == 0 || key0 > rows.last - p.c.window);
+                    if (!whole_tile) mask_tile(s_addr, t * kTileSlots, sg.k, pos, p.c.window, p.c.n_sink);
+                    if (__any_sync(0xffffffffu, off == -INFINITY)) {
+                        const float mx = tile_max(s_addr, 4);
+                        if (off == -INFINITY) off = mx * sc;
+                    }
+                    float sum = 0.f;
+                    uint32_t ra[32];
+                    ptx::tmem_ld_32x32b_x32(s_addr, ra);
+                    if (!take_turn()) { ok = false; break; }
+#pragma unroll 1
+                    for (int h = 0; h < 2;) {
+                        uint32_t pk[32], rb[32];
+                        const float o = (off == -INFINITY) ? 0.f : -off;
+                        const uint64_t no2 = pack2(o, o);
+                        uint64_t s0 = 0, s1 = 0;
+                        tmem_ld_wait32(ra);
+                        ptx::tmem_ld_32x32b_x32(s_addr + (uint32_t)(h * 64 + 32), rb);
+                        exp_chunk<false>(ra, sc2, no2, pk, s0, s1);
+                        tmem_ld_wait32(rb);
+                        ptx::tmem_ld_32x32b_x32(s_addr + 64, ra);    // (of no use to the second half)
+                        exp_chunk<false>(rb, sc2, no2, pk + 16, s0, s1);
+                        float a, b;
+                        unpack2(add2(s0, s1), a, b);
+                        const float half_sum = a + b;
+                        if (h == 1 && !redone) pass_turn();
+                        const bool grow = half_sum > kSumLimit && !redone;
+                        if (__any_sync(0xffffffffu, grow)) {
+                            tmem_ld_wait32(ra);
+                            if (h == 1) {
+                                if (!ptx::warp_wait(ctrl, &ctrl->pv_half[grp], s_par ^ 1, 69)) { ok = false; break; }
+                                ptx::tc_fence_after();
+                            }
+                            const float2 m = move_offset(s_addr + (uint32_t)(h * 64), o_addr, any_tile || h > 0 ? D : 0, grow, off, sc);
+                            off = m.x;
+                            l_run *= m.y;
+                            sum *= m.y;
+                            redone = true;
+                            ptx::tmem_ld_32x32b_x32(s_addr + (uint32_t)(h * 64), ra);
+                            continue;
+                        }
+                        redone = false;
+                        sum += half_sum;
+                        tmem_st_32x32b_x32(s_addr + (uint32_t)(h * 32), pk);
+                        tmem_st_wait();
+                        ptx::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(&ctrl->p_full[grp][h]);
+                        ++h;
+                    }
+                    if (!ok) break;
+                    tmem_ld_wait32(ra);
+                    l_run += sum;
+                } else {
+                    if (!take_turn()) { ok = false; break; }
+                    pass_turn();
+                    if (lane == 0) { ptx::mbar_arrive(&ctrl->p_full[grp][0]); ptx::mbar_arrive(&ctrl->p_full[grp][1]); }
+                }
+                any_tile |= on;
+            }
+            if (!ok) break;
+            // ---- end of this CTA's part of the unit
+            const bool whole = sg.t_first == 0 && sg.t_last == sg.tiles;
+            const size_t at = ((size_t)sg.layer * p.c.R + sg.u.row0 + tok) * p.c.Hq + kvh * p.c.G + hg;
+            __nv_bfloat16* const orow = p.c.out + at * D;
+            const int slot = sg.t_first > 0 ? 0 : 1;                 // a unit that began before this CTA's range uses slot 0
+            float* const rec = p.c.partial + (((size_t)blockIdx.x * 2 + slot) * 2 + grp) * kRowW * kRows + row;
+            left -= sg.t_last - sg.t_first;
+            if (!ptx::warp_wait(ctrl, &ctrl->o_full[grp], o_par, 70)) { ok = false; break; }
+            o_par ^= 1;
+            ptx::tc_fence_after();
+            if (warp_has_rows) {
+                const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+                const float w = off == -INFINITY || !any_tile ? 0.f : whole ? inv : 1.f;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t r[16];
+                    float acc[16];
+                    ptx::tmem_ld_32x32b_x16(o_addr + (uint32_t)c, r);
+                    tmem_ld_wait16(r);
+                    // (an accumulator that no P V wrote may hold anything: a weight of 0 does not read it)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[j] = w != 0.f ? w * __uint_as_float(r[j]) : 0.f;
+                    if (!whole) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) rec[(size_t)(c + j) * kRows] = acc[j];
+                    } else if (row_ok) {
+                        *reinterpret_cast<uint4*>(orow + c) = make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
+                        *reinterpret_cast<uint4*>(orow + c + 8) = make_uint4(pack_bf16(acc[8], acc[9]), pack_bf16(acc[10], acc[11]), pack_bf16(acc[12], acc[13]), pack_bf16(acc[14], acc[15]));
+                    }
+                }
+                if (!whole) {
+                    rec[(size_t)D * kRows] = any_tile ? off : -INFINITY;
+                    rec[(size_t)(D + 1) * kRows] = l_run;
+                } else if (p.c.lse_out && row_ok) {
+                    p.c.lse_out[at] = off * kAttnLn2 + logf(l_run);
+                }
+            }
+            // (the stream's next P V waits for a P that its own warps write after this)
+            ptx::tc_fence_before();
+            if (left > 0) next_segment(sg, p, n_cls, left);
+        }
+    }
+
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+// The units that the partition cut: one block per (inner boundary, stream).
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) attn_prompt_merge_kernel(const __grid_constant__ PromptParams p) {
+    const int grp = blockIdx.y;
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    merge_boundary<D>(
+        p.c.begins, p.n_cta, p.c.out, p.c.lse_out, p.c.status, p.c.wait_limit, 0,
+        [&](int row, const GroupBegin& u, size_t& place, size_t& lse_place) {
+            const PairClass c = load_class(p, u.b);
+            const int it = row / p.gs, hl = row - it * p.gs, kvh = u.g / p.shares, hg = (u.g - kvh * p.shares) * p.gs + hl, tok = c.tok + grp * p.nt + it;
+            place = lse_place = ((size_t)u.layer * p.c.R + c.row0 + tok) * p.c.Hq + kvh * p.c.G + hg;
+            return it < p.nt && tok < c.n && hg < p.c.G;
+        },
+        [&](int cta, int slot) { return p.c.partial + (((size_t)cta * 2 + slot) * 2 + grp) * (D + 4) * kRows; });
+}
+
+// Tokens of a row tile, and query heads: a group's heads, or (more than 128) an even share of them.
+void row_tile(int G, int* gs, int* shares, int* nt) {
+    *shares = (G + kRows - 1) / kRows;
+    *gs = (G + *shares - 1) / *shares;
+    *nt = kRows / *gs;
+}
+int most_classes(const mirror_ctx* ctx, int n_rows, int batch) {
+    int gs, shares, nt;
+    row_tile(ctx->desc.n_q_heads / ctx->desc.n_kv_heads, &gs, &shares, &nt);
+    return n_rows / (2 * nt) + batch + 1;
+}
+
+}  // namespace
+
+size_t mirror_attn_prompt_plan_bytes(const mirror_ctx* ctx, const mirror_rows* rows) {
+    return align_up(((size_t)ctx->num_sms + 1) * sizeof(CtaStart), 256) +
+           align_up((size_t)most_classes(ctx, rows->n_rows, rows->batch) * sizeof(PairClass), 256);
+}
+
+mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& cp, void* plan, cudaStream_t stream) {
+    const int D = ctx->desc.head_dim;
+    PromptParams p;
+    p.c = cp;
+    row_tile(cp.G, &p.gs, &p.shares, &p.nt);
+    p.n_hs = cp.Hkv * p.shares;
+    p.n_cta = ctx->num_sms;
+    p.max_classes = most_classes(ctx, cp.R, cp.B);
+    p.starts = (CtaStart*)plan;
+    p.classes = (PairClass*)((uint8_t*)plan + align_up(((size_t)ctx->num_sms + 1) * sizeof(CtaStart), 256));
+    if (p.n_cta + 1 > kPlanThreads || p.n_cta > 512 || (size_t)p.n_cta * sizeof(GroupBegin) > kWsNotesBytes) return MIRROR_ERR_SHAPE;
+    if ((int64_t)cp.L * cp.R > 0x7fffffff) return MIRROR_ERR_SHAPE;
+    Maps tm;
+    mirror_status st = mirror_attn_pool_tmap(ctx, kv, kv->k_pool, &tm.k);
+    if (st == MIRROR_OK) st = mirror_attn_pool_tmap(ctx, kv, kv->v_pool, &tm.v);
+    if (st != MIRROR_OK) return st;
+    {
+        // Q as (64 columns, heads, rows of all layers, D/64 halves): one box is one half of a row tile
+        const uint64_t row = (uint64_t)D * 2, rows = (uint64_t)cp.L * cp.R;
+        const uint64_t dims[5] = {64, (uint64_t)cp.Hq, rows, row / 128, 1};
+        const uint64_t strides[4] = {row, cp.Hq * row, 128, rows * cp.Hq * row};
+        const uint32_t box[5] = {64, (uint32_t)p.gs, (uint32_t)p.nt, 1, 1};
+        st = mirror_make_tmap(ctx, &tm.q, cp.q, 5, dims, strides, box);
+        if (st != MIRROR_OK) return st;
+    }
+    MIRROR_CUDA_OK(mirror_launch_pdl(attn_prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p));
+    auto launch = [&](auto cfg, auto kern, auto merge) -> mirror_status {
+        using C = decltype(cfg);
+        const size_t fixed = 2 * (size_t)C::kQBytes + kCtrlBytes;
+        const int stages = std::min((int)((kSmemLimit - fixed) / C::kStageBytes), kMaxStages);
+        MIRROR_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit));
+        MIRROR_CUDA_OK(mirror_launch_pdl(kern, dim3((unsigned)p.n_cta), dim3(kThreads), fixed + (size_t)stages * C::kStageBytes, stream, tm, p, stages));
+        MIRROR_CUDA_OK(cudaFuncSetAttribute(merge, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmem));
+        MIRROR_CUDA_OK(mirror_launch_pdl(merge, dim3((unsigned)(p.n_cta - 1), 2), dim3(kMergeThreads), kMergeSmem, stream, p));
+        return MIRROR_OK;
+    };
+    st = D == 128 ? launch(Cfg<128>{}, attn_prompt_kernel<128>, attn_prompt_merge_kernel<128>) : launch(Cfg<64>{}, attn_prompt_kernel<64>, attn_prompt_merge_kernel<64>);
+    if (st != MIRROR_OK) return st;
+    ctx->launches += 3;
+    MIRROR_CUDA_OK(cudaGetLastError());
+    return MIRROR_OK;
+}

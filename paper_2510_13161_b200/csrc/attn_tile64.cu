@@ -875,11 +875,12 @@ __global__ void __launch_bounds__(attn::kMergeThreads) attn_tile64_merge_kernel(
     ptx::grid_dep_launch();                       // (the kernel behind only sets itself up before this one has completed)
     ptx::grid_dep_wait();
     attn::merge_boundary<D>(
-        p.begins, p.n_groups, p.n, p.Hq, p.B, p.out, p.lse_out, p.status, p.wait_limit, p.stall_merge,
-        [&](int row, const attn::GroupBegin& u, int& node, int& head) {
-            const int r_abs = rb * p.rows_per_rb + row;
-            node = r_abs / p.G;
-            head = u.g * p.G + r_abs % p.G;
+        p.begins, p.n_groups, p.out, p.lse_out, p.status, p.wait_limit, p.stall_merge,
+        [&](int row, const attn::GroupBegin& u, size_t& place, size_t& lse_place) {
+            const int r_abs = rb * p.rows_per_rb + row, node = r_abs / p.G, head = u.g * p.G + r_abs % p.G;
+            const size_t lb = (size_t)u.layer * p.B + u.b;
+            place = (lb * p.n + node) * (size_t)p.Hq + head;
+            lse_place = (lb * p.Hq + head) * p.n + node;
             return row < p.rows_per_rb && r_abs < p.rows;
         },
         [&](int group, int slot) { return p.partial + ((size_t)(group * p.n_rb + rb) * 2 + slot) * (D + 4) * kRows; });

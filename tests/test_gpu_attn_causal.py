@@ -48,10 +48,50 @@ def test_a_scale_of_its_own_and_uniform_rows():
     check_attention(make(4, 2, 64, scale=0.3), Case(4, 2, 64, [33, 70, 5], [2, 2, 2], seed=7, uniform=True), False, scale=0.3)
 
 
+COUNTS = [1, 100, 16, 0, 300, 33, 128, 15, 257, 64]
+
+
+@pytest.mark.parametrize("hq,hkv", [(4, 4), (8, 2), (5, 1), (14, 2), (32, 1), (144, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts(hq, hkv, d):
+    check_attention(make(hq, hkv, d), Case(hq, hkv, d, LENS, COUNTS, pad=2, seed=hq), True)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 0), (17, 16), (40, 3), (100, 33), (100, 200), (300, 0), (5000, 4)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts_under_a_window(window, sinks, d):
+    check_attention(make(8, 2, d), Case(8, 2, d, LENS, COUNTS, window=window, sinks=sinks, seed=window), True)
+    check_attention(make(2, 2, d), Case(2, 2, d, [0, 700, 33], [400, 129, 256], window=window, sinks=sinks, seed=window + 1), True)
+
+
+def test_prompts_of_every_length_around_a_tile():
+    for n in (17, 31, 32, 33, 63, 64, 65, 127, 128, 129):
+        check_attention(make(4, 1, 64), Case(4, 1, 64, [n, 0, 128 - n % 128], [n, n + 1, 1], seed=n), True)
+
+
+def test_a_prompt_cut_over_all_ctas_and_several_layers():
+    check_attention(make(8, 1, 128), Case(8, 1, 128, [9000], [40], seed=1), True)
+    check_attention(make(8, 2, 64), Case(8, 2, 64, [5000, 3, 0], [50, 600, 1], layers=3, seed=2), True)
+    check_attention(make(4, 4, 128), Case(4, 4, 128, [0], [1500], seed=3), True)
+
+
+def test_many_requests_with_prompts():
+    check_attention(make(4, 1, 64), Case(4, 1, 64, [(b * 13) % 90 for b in range(1024)], [(b * 5) % 11 for b in range(1024)], seed=3), True)
+
+
+@pytest.mark.parametrize("spread", [8.0, 0.0])
+def test_prompts_with_scores_far_apart_and_all_alike(spread):
+    check_attention(make(8, 2, 128), Case(8, 2, 128, [700, 40], [70, 200], seed=6, spread=spread), True)
+
+
 def test_twice_and_on_another_stream_the_same():
     m = make(8, 2, 128)
-    c = Case(8, 2, 128, [3000, 77], [1, 1], seed=8)
-    a, la = check_attention(m, c, False)
+    for counts in ([1, 1], [40, 300]):
+        again(m, Case(8, 2, 128, [3000, 77], counts, seed=8), counts[0] > 1)
+
+
+def again(m, c, p_rounded):
+    a, la = check_attention(m, c, p_rounded)
     s = torch.cuda.Stream()
     out, lse = torch.empty_like(a), torch.empty_like(la)
     q = c.q.cuda()
@@ -62,19 +102,20 @@ def test_twice_and_on_another_stream_the_same():
     assert torch.equal(a, out) and torch.equal(la, lse)
 
 
-def test_captured_and_replayed_with_other_lengths():
+@pytest.mark.parametrize("n", [1, 30])
+def test_captured_and_replayed_with_other_lengths(n):
     """The partition is made on the device: a captured call follows the lengths that it finds."""
     m = make(8, 2, 128)
-    c = Case(8, 2, 128, [1500, 900], [1, 1], seed=9)
+    c = Case(8, 2, 128, [1500, 900], [n, n], seed=9)
     kv, rows = c.device(m)
-    q, out = c.q.cuda(), torch.empty((1, 2, 8, 128), dtype=torch.bfloat16, device="cuda")
+    q, out = c.q.cuda(), torch.empty((1, 2 * n, 8, 128), dtype=torch.bfloat16, device="cuda")
     m.mirror_attn_causal(kv, rows, q, out=out)
     torch.cuda.synchronize()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         m.mirror_attn_causal(kv, rows, q, out=out)
     lens = kv._refs[3]
-    for a, b in ((1500, 900), (3, 899), (0, 17)):
+    for a, b in ((1500, 900), (3, 870), (0, 17)):
         lens.copy_(torch.tensor([a, b], dtype=torch.int32))
         g.replay()
         got = out.clone()
@@ -84,9 +125,10 @@ def test_captured_and_replayed_with_other_lengths():
     assert m.device_status() == (0, 0)
 
 
-def test_reports():
+@pytest.mark.parametrize("n", [1, 20])
+def test_reports(n):
     m = make(4, 2, 64)
-    c = Case(4, 2, 64, [20, 5], [1, 1], seed=1)
+    c = Case(4, 2, 64, [20, 5], [n, n], seed=1)
     kv, rows = c.device(m)
     q = c.q.cuda()
     lens, table = kv._refs[3], kv._refs[2]
@@ -99,7 +141,7 @@ def test_reports():
         torch.cuda.synchronize()
         assert m.device_status() == (6, code), name
         lens.copy_(kept[0]), table.copy_(kept[1])
-    rows._refs[0].copy_(torch.tensor([0, 2, 1], dtype=torch.int32))          # a request with more rows than max_rows
+    rows._refs[0].copy_(torch.tensor([0, n + 1, n], dtype=torch.int32))          # a request with more rows than max_rows
     table[table > 90] = 0
     m.mirror_attn_causal(kv, rows, q)
     torch.cuda.synchronize()
