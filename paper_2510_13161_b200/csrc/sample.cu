@@ -13,7 +13,8 @@
 //      bin's mass to 10^-4.  With Top-p over the whole row also the exact total
 //   3  the leading CTA reads off a bin that surely lies behind the end of the front
 //   4  if at most kList ids lie ahead of that, they all go to the leader, which sorts them and does the rest: the usual case
-//   4' otherwise the front's end is found by bisection over the logits' ordered keys, with exact counts and masses of each half
+//   4' otherwise only the bin in which the front ends goes to the leader, which sorts it; what lies ahead of it is counted and summed by all.
+//      (A bin of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
 //   5  the drawn token, by the warps' masses, and the filtered distribution
 // What bounds it: double-precision arithmetic (18 operations an id, 64 a cycle and SM) where Top-p or a draw takes the whole row, the
 // bytes otherwise; for a row alone the cluster's barriers.
@@ -56,13 +57,14 @@ struct SampleParams {
 };
 
 // What the CTAs of a cluster tell one another, and what a CTA's warps share.
-struct Shared {
+struct alignas(16) Shared {
     float max[kMaxCluster];
-    u64 sum[2][kMaxCluster][2];               // (count, mass) of the CTAs, for steps in turns
-    u64 warp_sum[kWarps][2];
+    u64 sum[2][kMaxCluster][3];               // sums of the CTAs, for steps in turns
+    u64 warp_sum[kWarps][3];
     u64 warp_mass[kWarps];                    // kept mass of the warps' parts
     u64 total;                                // the row's mass
     int last_bin, n_list, list_at;            // written by the leader
+    int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
     u64 cut_key;                              // composite key of the last kept id
     u64 kept;                                 // its front's mass
     int drawn, n;
@@ -75,6 +77,8 @@ struct Shared {
     };
     u64 mass[kList];
 };
+
+static_assert(sizeof(Shared) % 16 == 0, "the logits behind it are read 16 bytes at a time");
 
 __device__ __forceinline__ float unkey(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 
@@ -127,6 +131,25 @@ __device__ __forceinline__ u64 warp_incl64(u64 v) {
         if (lane >= o) v += t;
     }
     return v;
+}
+
+// The first n entries of the list in ascending order (bitonic, by the whole block).
+__device__ __noinline__ void sort_list(Shared& s, int n) {
+    const int tid = threadIdx.x;
+    int n2 = 32;
+    while (n2 < n) n2 <<= 1;
+    __syncthreads();
+    for (int i = n + tid; i < n2; i += kThreads) s.list[i] = ~0ull;
+    for (int size = 2; size <= n2; size <<= 1)
+        for (int d = size >> 1; d; d >>= 1) {
+            __syncthreads();
+            for (int t = tid; t < n2 / 2; t += kThreads) {
+                const int i = ((t & ~(d - 1)) << 1) | (t & (d - 1)), j = i | d;
+                const u64 a = s.list[i], b = s.list[j];
+                if ((a > b) == ((i & size) == 0)) { s.list[i] = b; s.list[j] = a; }
+            }
+        }
+    __syncthreads();
 }
 
 __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant__ SampleParams p) {
@@ -207,29 +230,33 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
     // composite key of an id: smaller is ahead
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
     int turn = 0;
-    // (count, mass) over the cluster of what f(i) gives for the ids of the part; every thread gets both
-    auto all_sums = [&](auto f, u64& n, u64& m) {
-        n = m = 0;
+    // Sums over the cluster of what f(l, i, sums) adds for the ids of the part; every thread gets them.
+    struct Sums {
+        u64 n, m, o;
+    };
+    auto all_sums = [&](auto f) -> Sums {
+        Sums a = {0, 0, 0};
         for (int i = w0 + lane * 4; i < w1; i += 128) {
             const float4 v = *reinterpret_cast<const float4*>(z + i);
-            f(v.x, i, n, m); f(v.y, i + 1, n, m); f(v.z, i + 2, n, m); f(v.w, i + 3, n, m);
+            f(v.x, i, a); f(v.y, i + 1, a); f(v.z, i + 2, a); f(v.w, i + 3, a);
         }
-        n = warp_sum64(n);
-        m = warp_sum64(m);
+        a.n = warp_sum64(a.n);
+        a.m = warp_sum64(a.m);
+        a.o = warp_sum64(a.o);
         __syncthreads();
-        if (lane == 0) { s.warp_sum[warp][0] = n; s.warp_sum[warp][1] = m; }
+        if (lane == 0) { s.warp_sum[warp][0] = a.n; s.warp_sum[warp][1] = a.m; s.warp_sum[warp][2] = a.o; }
         __syncthreads();
-        if (tid < C) {
-            u64 a = 0, b = 0;
-            for (int w = 0; w < kWarps; ++w) { a += s.warp_sum[w][0]; b += s.warp_sum[w][1]; }
-            Shared* const o = cluster.map_shared_rank(&s, tid);
-            o->sum[turn][rank][0] = a;
-            o->sum[turn][rank][1] = b;
+        if (tid < 3 * C) {
+            const int c = tid / 3, k = tid - c * 3;
+            u64 t = 0;
+            for (int w = 0; w < kWarps; ++w) t += s.warp_sum[w][k];
+            cluster.map_shared_rank(&s, c)->sum[turn][rank][k] = t;
         }
         cluster.sync();
-        n = m = 0;
-        for (int c = 0; c < C; ++c) { n += s.sum[turn][c][0]; m += s.sum[turn][c][1]; }
+        a = {0, 0, 0};
+        for (int c = 0; c < C; ++c) { a.n += s.sum[turn][c][0]; a.m += s.sum[turn][c][1]; a.o += s.sum[turn][c][2]; }
         turn ^= 1;                                               // (read before the other turn's barrier: rewritten after it)
+        return a;
     };
 
     u64 cut = ~0ull;                                             // composite key of the last id of the front
@@ -241,7 +268,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             at = weigh.max_inf ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));
             return (int)at;
         };
-        const bool whole_total = by_p && !by_k;
+        const bool whole_total = by_p && !by_k;                  // Top-p of the whole row
         for (int i = w0 + lane * 4; i < w1; i += 128) {
             const float4 v4 = *reinterpret_cast<const float4*>(z + i);
             const float v[4] = {v4.x, v4.y, v4.z, v4.w};
@@ -251,10 +278,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 float at;
                 const int bin = bin_of(v[j], at);
                 atomicAdd(&s.hist[bin], 1u);
-                if (whole_total) {
-                    atomicAdd(&s.off[bin], (uint32_t)((at - (float)bin) * 1024.f));
-                    total += weigh(v[j]);
-                }
+                if (by_p) atomicAdd(&s.off[bin], (uint32_t)((at - (float)bin) * 1024.f));
+                if (whole_total) total += weigh(v[j]);
             }
         }
         total = warp_sum64(total);
@@ -270,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 const uint32_t n = s.hist[i];
                 if (n) {
                     atomicAdd(&lead->hist[i], n);
-                    if (whole_total) atomicAdd(&lead->off[i], s.off[i]);
+                    if (by_p) atomicAdd(&lead->off[i], s.off[i]);
                 }
             }
         cluster.sync();
@@ -286,7 +311,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 const int b = tid * kPer + j;
                 cnt[j] = s.hist[b];
                 ms[j] = 0.0;
-                if (cnt[j] && whole_total) {
+                if (cnt[j] && by_p) {
                     // (the mean of exp(-x) over a 64th is exp(-mean) but for a relative x^2 / 2 of 10^-4; the last bin is open: no mass)
                     const float mean = ((float)b + (float)s.off[b] * (1.f / 1024.f) / (float)cnt[j]) * (1.f / kBinsPerNat);
                     ms[j] = b == kBins - 1 ? 0.0 : (double)cnt[j] * (double)expf(-mean);
@@ -304,16 +329,33 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             }
             if (lane == 31) { s.warp_sum[warp][0] = n_in; s.warp_sum[warp][1] = (u64)__double_as_longlong(m_in); }
             if (tid == 0) {
-                s.last_bin = kBins - 1;
+                s.last_bin = s.bin_k = s.bin_p = kBins - 1;
                 u64 a = 0;
                 for (int c = 0; c < C; ++c) a += s.sum[0][c][0];
                 s.total = a;
             }
             __syncthreads();
             for (int w = 0; w < warp; ++w) { n_in += s.warp_sum[w][0]; m_in += __longlong_as_double((long long)s.warp_sum[w][1]); }
-            const double want = whole_total ? top_p * (double)s.total * exp2(-(double)p.shift) * 1.002 : 0.0;
             u64 nb = n_in - n;
             double mb = m_in - m;
+            // Top-k's bin, and about what its front weighs
+            if (by_k) {
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    if (nb < (u64)k && nb + cnt[j] >= (u64)k) {
+                        s.bin_k = tid * kPer + j;
+                        s.warp_mass[0] = (u64)__double_as_longlong(mb + ms[j] * (double)(k - (int)nb) / (double)cnt[j]);
+                    }
+                    nb += cnt[j];
+                    mb += ms[j];
+                }
+                if (tid == kThreads - 1 && nb < (u64)k) s.warp_mass[0] = (u64)__double_as_longlong(mb);
+                __syncthreads();
+                nb = n_in - n;
+                mb = m_in - m;
+            }
+            const double row_mass = by_k ? __longlong_as_double((long long)s.warp_mass[0]) : (double)s.total * exp2(-(double)p.shift);
+            const double about = by_p ? top_p * row_mass : 0.0, want = whole_total ? about * 1.002 : 0.0;
             // (Top-p behind Top-k is a share of all that Top-k leaves: then Min-p does not shorten the list)
             const float m_at = -logf((float)fmin(min_p, 1.0)) * kBinsPerNat + 1.f;
             const bool m_ends = by_m && !(by_k && by_p);
@@ -325,6 +367,14 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 if ((by_k && nb >= (u64)k) || (whole_total && mb >= want) || (m_ends && (float)(tid * kPer + j) >= m_at)) {
                     atomicMin(&s.last_bin, tid * kPer + j);
                     break;
+                }
+            }
+            mb = m_in - m;
+            if (by_p) {
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    mb += ms[j];
+                    if (mb >= about) { atomicMin(&s.bin_p, tid * kPer + j); break; }
                 }
             }
             __syncthreads();
@@ -339,6 +389,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             if (tid < C) {
                 Shared* const o = cluster.map_shared_rank(&s, tid);
                 o->last_bin = s.last_bin;
+                o->bin_k = s.bin_k;
+                o->bin_p = s.bin_p;
                 o->n_list = s.n_list;
                 o->total = s.total;
             }
@@ -362,22 +414,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             }
             cluster.sync();
             if (rank == 0) {
-                int n2 = 32;
-                while (n2 < n_list) n2 <<= 1;
-                for (int i = n_list + tid; i < n2; i += kThreads) s.list[i] = ~0ull;
-                auto sort = [&]() {                              // bitonic, ascending
-                    for (int size = 2; size <= n2; size <<= 1)
-                        for (int d = size >> 1; d; d >>= 1) {
-                            __syncthreads();
-                            for (int t = tid; t < n2 / 2; t += kThreads) {
-                                const int i = ((t & ~(d - 1)) << 1) | (t & (d - 1)), j = i | d;
-                                const u64 a = s.list[i], b = s.list[j];
-                                if ((a > b) == ((i & size) == 0)) { s.list[i] = b; s.list[j] = a; }
-                            }
-                        }
-                    __syncthreads();
-                };
-                sort();
+                sort_list(s, n_list);
                 constexpr int kPer = kList / kThreads;
                 // inclusive sums of mass[] over the list: a thread has neighbours
                 auto scan = [&](u64 (&w)[kPer], u64& before) -> u64 {
@@ -434,8 +471,6 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 }
                 // the draw: the kept ids in their own order (id, then the key's place in the list)
                 __syncthreads();
-                n2 = 32;
-                while (n2 < n) n2 <<= 1;
                 u64 by_id[kPer];
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
@@ -444,9 +479,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 }
                 __syncthreads();
 #pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (tid + j * kThreads < n2) s.list[tid + j * kThreads] = by_id[j];
-                sort();
+                for (int j = 0; j < kPer; ++j) s.list[tid + j * kThreads] = by_id[j];
+                sort_list(s, n);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
                     const int r = tid * kPer + j;
@@ -472,38 +506,117 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             cut = s.cut_key;
             total = s.kept;
         } else {
-            // ---- 4': bisection over composite keys, by bits from above
-            u64 n_all, m_all;
-            auto front = [&](u64 at, u64& n, u64& m) {           // ids up to the composite key `at`
-                all_sums([&](float l, int i, u64& cn, u64& cm) {
-                    if (may(l) && key_of(l, first + i) <= at) { ++cn; cm += weigh(l); }
-                }, n, m);
+            // ---- 4': the bin in which each filter's front ends, and where in it
+            auto front = [&](u64 at) {                           // (count, mass) of the ids up to the composite key `at`
+                return all_sums([&](float l, int i, Sums& a) {
+                    if (may(l) && key_of(l, first + i) <= at) { ++a.n; a.m += weigh(l); }
+                });
             };
-            // the smallest key whose front fulfils `done` (monotone)
-            auto search = [&](u64 hi, auto done) -> u64 {
-                u64 lo = 0;
+            // the least order key that lies in bin b or ahead of it (no data takes part)
+            auto edge = [&](int b) -> uint32_t {
+                uint32_t lo = 0, hi = mirror_order_key(mx);
                 while (lo < hi) {
-                    const u64 mid = lo + ((hi - lo) >> 1);
-                    u64 n, m;
-                    front(mid, n, m);
-                    if (done(n, m)) hi = mid; else lo = mid + 1;
+                    const uint32_t mid = lo + ((hi - lo) >> 1);
+                    float at;
+                    if (bin_of(unkey(mid), at) <= b) hi = mid; else lo = mid + 1;
                 }
                 return lo;
             };
+            // The smallest key whose front (count, mass) fulfils `done`, which is monotone; guessed to lie in bin `b`.
+            auto end_of = [&](int b, bool by_mass, auto done) -> u64 {
+                u64 n0, m0, n_in;
+                for (;;) {
+                    // what lies ahead of the bin, and the bin itself into the leader's list
+                    if (rank == 0 && tid == 0) s.list_at = 0;
+                    cluster.sync();
+                    const Sums a = all_sums([&](float l, int i, Sums& a) {
+                        if (!may(l)) return;
+                        float at;
+                        const int bin = bin_of(l, at);
+                        if (bin > b) return;
+                        const u64 w = by_mass ? weigh(l) : 0ull;
+                        if (bin < b) {
+                            ++a.n;
+                            a.m += w;
+                        } else {
+                            a.n += 1ull << 32;
+                            a.o += w;
+                            const int slot = atomicAdd(&lead->list_at, 1);
+                            if (slot < kList) lead->list[slot] = key_of(l, first + i);
+                        }
+                    });
+                    n0 = a.n & 0xffffffffull;
+                    n_in = a.n >> 32;
+                    m0 = a.m;
+                    if (n0 > 0 && done(n0, m0)) { --b; continue; }                                // it ends ahead of this bin
+                    if (b < kBins - 1 && !done(n0 + n_in, m0 + a.o)) { ++b; continue; }           // ... or behind it
+                    break;
+                }
+                if (n_in > (u64)kList) {
+                    u64 lo = b > 0 ? (u64)~(edge(b - 1) - 1) << 32 : 0ull, hi = ((u64)~edge(b) << 32) | 0xffffffffull;
+                    while (lo < hi) {
+                        const u64 mid = lo + ((hi - lo) >> 1);
+                        const Sums a = front(mid);
+                        if (done(a.n, a.m)) hi = mid; else lo = mid + 1;
+                    }
+                    return lo;
+                }
+                if (rank == 0) {
+                    const int n = (int)n_in;
+                    sort_list(s, n);
+                    constexpr int kPer = kList / kThreads;
+                    u64 w[kPer], mine = 0;
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        const int r = tid * kPer + j;
+                        w[j] = by_mass && r < n ? weigh(unkey(~(uint32_t)(s.list[r] >> 32))) : 0ull;
+                        mine += w[j];
+                    }
+                    u64 at = warp_incl64(mine);
+                    __syncthreads();
+                    if (lane == 31) s.warp_sum[warp][0] = at;
+                    if (tid == 0) s.list_at = n - 1;
+                    __syncthreads();
+                    at += m0 - mine;
+                    for (int q = 0; q < warp; ++q) at += s.warp_sum[q][0];
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        const int r = tid * kPer + j;
+                        at += w[j];
+                        if (r < n && done(n0 + r + 1, at)) { atomicMin(&s.list_at, r); break; }
+                    }
+                    __syncthreads();
+                    if (tid < C) cluster.map_shared_rank(&s, tid)->cut_key = s.list[s.list_at];
+                }
+                cluster.sync();
+                const u64 c = s.cut_key;
+                cluster.sync();                                  // (the next one may be written)
+                return c;
+            };
             if (by_k) {
-                cut = search(~0ull, [&](u64 n, u64) { return n >= (u64)k; });
-                if (by_p) front(cut, n_all, total);
+                cut = end_of(s.bin_k, false, [&](u64 n, u64) { return n >= (u64)k; });
+                if (by_p) total = front(cut).m;
             }
             if (by_p) {
                 const double want = top_p * (double)total;
-                const u64 c = search(cut, [&](u64 n, u64 m) { return n >= 1 && (double)m >= want; });
+                const u64 c = end_of(s.bin_p, true, [&](u64 n, u64 m) { return n >= 1 && (double)m >= want; });
                 cut = min(cut, c);
             }
             if (by_m) {
-                // (the last key of at least min_w: the front that holds all of them)
-                all_sums([&](float l, int i, u64& cn, u64&) { if (may(l) && key_of(l, first + i) <= cut && weigh(l) >= min_w) ++cn; }, n_all, m_all);
-                const u64 want = max(n_all, (u64)1);
-                cut = search(cut, [&](u64 n, u64) { return n >= want; });
+                // the last logit of at least min_w, by its key (no data takes part)
+                __syncthreads();
+                if (warp == 0) {
+                    uint32_t lo = 0, hi = mirror_order_key(mx);  // weight(hi) >= min_w
+                    while (lo < hi) {
+                        const uint32_t mid = lo + ((hi - lo) >> 1);
+                        const float l = unkey(mid);
+                        if (l > -INFINITY && weigh(l) >= min_w) hi = mid; else lo = mid + 1;
+                    }
+                    if (lane == 0) s.warp_mass[0] = ((u64)~hi << 32) | 0xffffffffull;
+                }
+                __syncthreads();
+                cut = min(cut, s.warp_mass[0]);
+                __syncthreads();
             }
         }
     }
