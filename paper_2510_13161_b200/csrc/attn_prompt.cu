@@ -7,10 +7,12 @@
 // the window of its first row to its last row; eight slots to a tile of 128 keys.  What no row of a stream sees of a tile is neither
 // multiplied nor exponentiated.
 //
-// The tiles of all units form one sequence that is split evenly over the CTAs, one per SM: prompts are causal, so units are of any
-// length, and a few short requests behind a long prefix are few units.  attn_prompt_plan_kernel counts the tiles (they depend on lengths
-// that only the device knows) and finds where each CTA begins; a unit that a boundary cuts leaves a (max, sum, accumulator) record per
-// part and stream, which attn_prompt_merge_kernel combines in the order of the parts.
+// Units are of any length (prompts are causal), and how many tiles they have only the device knows.  Every CTA, one per SM, makes the same
+// plan for itself, in the ring's shared memory, and takes its part:
+//   whole  units sorted by length are dealt out in turns, there and back (the longest go with the shortest): nothing is cut
+//   cut    the tiles of all units form one sequence that is split evenly.  A unit that a boundary cuts leaves a (max, sum,
+//          accumulator) record per part and stream, which attn_prompt_merge_kernel combines in the order of the parts
+// whichever ends sooner, a cut counted as kCutTiles and a unit's start and end as kUnitTiles.
 //
 // Per CTA, 12 warps (as in attn_verify.cu, whose softmax this shares; see there for the offset that stands in for a running maximum):
 //   warps 0, 3   stage K and V tiles into one ring; the V warp stages Q too
@@ -37,25 +39,21 @@ constexpr int kRows = 128;                          // UMMA M: rows of a stream
 constexpr int kMaxStages = 10;
 constexpr int kTmemCols = 512;
 constexpr int kTmemO = 2 * kTileTok;
-constexpr int kCtrlBytes = 512;
+constexpr int kCtrlBytes = 1536;
 constexpr size_t kSmemLimit = 232448;               // 227 KB
-constexpr int kPlanThreads = 1024;
 constexpr int kSnapTiles = 2;                       // a boundary moves to a unit boundary that is at most this many tiles away
+constexpr int kUnitTiles = 1;                       // what a unit costs beside its tiles
+constexpr int kCutTiles = 6;                        // what cutting costs: a record, a unit more, the merge behind
+constexpr int kMaxList = 24;                        // whole units of a CTA
+constexpr int kMaxSorted = kThreads;                // pairs that are sorted
 
-// One pair of row tiles of one request, the same for all layers and heads.
-struct PairClass {
+// A unit: a pair of row tiles of one request, of one layer and head.
+struct Unit {
     int row0, n, prefix;                  // the request's rows
     int tok;                              // the pair's first token
-    int tiles, cum;                       // K/V tiles; tiles of the classes before it
-    int b, pad;
+    int b, layer, hs, tiles;              // hs: KV head (x share of its query heads); K/V tiles
 };
-// Where a CTA begins, and how many tiles it has.
-struct CtaStart {
-    int layer, hs, cls, t;
-    int n_tiles;
-    int pad[3];
-};
-static_assert(sizeof(PairClass) == 32 && sizeof(CtaStart) == 32, "two 16-byte loads each");
+static_assert(sizeof(Unit) == 32, "32 bytes");
 
 struct PromptParams {
     CausalParams c;
@@ -63,9 +61,8 @@ struct PromptParams {
     int nt;                               // tokens of a row tile
     int n_hs;                             // KV heads x shares
     int n_cta;
-    int max_classes;
-    PairClass* classes;
-    CtaStart* starts;                     // [n_cta + 1] (the last one's cls: how many classes there are)
+    int wide_out;                         // out on a 32-byte boundary
+    Unit* firsts;                         // [n_cta] the unit that each CTA's range begins in, for the merge
 };
 
 struct Maps {
@@ -88,7 +85,74 @@ __device__ __forceinline__ Keys pair_keys(const PromptParams& p, int n, int pref
     return k;
 }
 
-// ---- the plan: one block ---------------------------------------------------------------------------------------
+// ---- a CTA's way through its units -----------------------------------------------------------------------------
+struct Ctrl;
+struct Segment {
+    Unit u;
+    int t_first, t_last;                  // tiles [t_first, t_last) of the unit
+    int k;                                // (whole units) place in the CTA's list
+    Keys keys;
+};
+__device__ __forceinline__ int tiles_of(const PromptParams& p, int n, int prefix, int tok) {
+    return (pair_keys(p, n, prefix, tok).slots + kTileSlots - 1) / kTileSlots;
+}
+__device__ __forceinline__ void fill_segment(Segment& s, const PromptParams& p, int left) {
+    s.t_last = min(s.u.tiles, s.t_first + left);
+    s.keys = pair_keys(p, s.u.n, s.u.prefix, s.u.tok);
+}
+// Does some row of stream g see something of tile t?  (Its tokens are tok + g nt and the nt - 1 behind it, as far as they exist.)
+struct StreamRows {
+    int first, last;                      // positions; last < first: no rows
+};
+__device__ __forceinline__ StreamRows stream_rows(const PromptParams& p, const Segment& s, int g) {
+    const int t0 = s.u.tok + g * p.nt, t1 = min(t0 + p.nt, s.u.n) - 1;
+    return {s.u.prefix + t0, s.u.prefix + t1};
+}
+__device__ __forceinline__ bool tile_seen(const PromptParams& p, const Segment& s, const StreamRows& r, int t) {
+    const int key0 = s.keys.page(t * kTileSlots) * kSlotTok, key1 = s.keys.page(min(t * kTileSlots + kTileSlots, s.keys.slots) - 1) * kSlotTok + kSlotTok - 1;
+    return r.last >= r.first && key0 <= r.last && (p.c.window == 0 || key1 > r.first - p.c.window || key0 < p.c.n_sink);
+}
+
+struct Ctrl {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t q_full, q_empty;
+    uint64_t s_full[2], p_full[2][2], o_full[2];        // per stream (P: per half of the tile)
+    uint64_t pv_half[2];
+    uint64_t turn[2];                                   // the issuing warps take turns
+    uint64_t exp_turn[2][4];                            // the two softmax warps of a scheduler take turns
+    Unit first;                                         // where this CTA begins
+    int first_t, n_tiles, whole, n_list;
+    int makespan, ends[2];
+    int scan[kThreads / 32];
+    int* status;
+    long long wait_limit;
+    uint32_t tmem_base;
+    volatile int abort;
+    Unit list[kMaxList];                                // its units, where they are dealt out whole
+};
+static_assert(sizeof(Ctrl) <= kCtrlBytes, "control block");
+
+// On to the next unit (there is one).
+__device__ __noinline__ void next_segment(Segment& s, const PromptParams& p, const Ctrl* ctrl, int left) {
+    s.t_first = 0;
+    if (ctrl->whole) {
+        s.u = ctrl->list[++s.k];
+    } else {
+        s.u.tok += 2 * p.nt;
+        while (s.u.tok >= s.u.n) {                       // (requests without rows are passed over)
+            s.u.tok = 0;
+            if (++s.u.b == p.c.B) {
+                s.u.b = 0;
+                if (++s.u.hs == p.n_hs) { s.u.hs = 0; ++s.u.layer; }
+            }
+            causal::load_request(p.c, s.u.b, s.u.row0, s.u.n, s.u.prefix, false);
+        }
+        s.u.tiles = tiles_of(p, s.u.n, s.u.prefix, s.u.tok);
+    }
+    fill_segment(s, p, left);
+}
+
+// ---- the plan: every CTA for itself ----------------------------------------------------------------------------
 __device__ int block_scan(int v, int* s_warp, int* total) {              // inclusive, over the block
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -100,169 +164,198 @@ __device__ int block_scan(int v, int* s_warp, int* total) {              // incl
     if (lane == 31) s_warp[warp] = v;
     __syncthreads();
     int before = 0, all = 0;
-    for (int w = 0; w < kPlanThreads / 32; ++w) {
+    for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) before += s_warp[w];
         all += s_warp[w];
     }
     *total = all;
     return v + before;
 }
-__global__ void __launch_bounds__(kPlanThreads) attn_prompt_plan_kernel(const __grid_constant__ PromptParams p) {
-    __shared__ int s_base[kAttnMaxBatch + 1], s_row0[kAttnMaxBatch], s_n[kAttnMaxBatch], s_prefix[kAttnMaxBatch], s_warp[kPlanThreads / 32];
-    __shared__ int s_at[kPlanThreads];                   // where the CTAs begin in the sequence
-    ptx::grid_dep_wait();
-    ptx::grid_dep_launch();
-    const int tid = threadIdx.x;
-    int n_cls = 0;
-    {
-        int pairs = 0;
-        if (tid < p.c.B) {
-            int row0, n, prefix;
-            causal::load_request(p.c, tid, row0, n, prefix, true);
-            s_row0[tid] = row0; s_n[tid] = n; s_prefix[tid] = prefix;
-            pairs = (n + 2 * p.nt - 1) / (2 * p.nt);
+// Scratch in shared memory: pairs summed over the requests, and the requests' rows.
+struct Scratch {
+    int *base, *row0, *n, *prefix;        // [B + 1], [B] each
+    int *sorted, *sorted_tiles;           // [kMaxSorted]: pairs by length
+};
+__device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* mem) {
+    const int tid = threadIdx.x, lane = tid & 31, B = p.c.B, cta = blockIdx.x;
+    Scratch x;
+    x.sorted = mem;
+    x.sorted_tiles = x.sorted + kMaxSorted;
+    x.base = x.sorted_tiles + kMaxSorted;
+    x.row0 = x.base + B + 1;
+    x.n = x.row0 + B;
+    x.prefix = x.n + B;
+    for (int b = tid; b < B; b += kThreads) {
+        int row0, n, prefix;
+        causal::load_request(p.c, b, row0, n, prefix, cta == 0);
+        x.row0[b] = row0; x.n[b] = n; x.prefix[b] = prefix;
+        x.base[b + 1] = (n + 2 * p.nt - 1) / (2 * p.nt);
+    }
+    if (tid == 0) { x.base[0] = 0; ctrl->makespan = 0; ctrl->n_tiles = 0; ctrl->whole = 0; ctrl->n_list = 0; }
+    __syncthreads();
+    if (tid < 32) {
+        int acc = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            int v = b0 + lane < B ? x.base[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int t = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += t;
+            }
+            if (b0 + lane < B) x.base[b0 + lane + 1] = acc + v;
+            acc += __shfl_sync(0xffffffffu, v, 31);
         }
-        const int incl = block_scan(pairs, s_warp, &n_cls);
-        if (tid < p.c.B) s_base[tid + 1] = incl;
-        if (tid == 0) s_base[0] = 0;
     }
     __syncthreads();
-    if (n_cls > p.max_classes) {                         // (overlapping requests: more rows than there are)
-        if (tid == 0) causal::report(p.c.status, MIRROR_DEV_CHECK, 830);
-        n_cls = 0;
+    const int pairs = x.base[B];
+    if (pairs == 0) {
+        if (tid == 0) p.c.begins[cta] = {0, 0, 0, 0};
+        return;
     }
-    int total = 0;
-    for (int c0 = 0; c0 < n_cls; c0 += kPlanThreads) {
-        const int c = c0 + tid;
-        PairClass u = {};
-        if (c < n_cls) {
-            int lo = 0, hi = p.c.B - 1;                  // the first b with s_base[b + 1] > c
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (s_base[mid + 1] > c) hi = mid; else lo = mid + 1;
-            }
-            u.b = lo;
-            u.row0 = s_row0[lo]; u.n = s_n[lo]; u.prefix = s_prefix[lo];
-            u.tok = (c - s_base[lo]) * 2 * p.nt;
-            u.tiles = max((pair_keys(p, u.n, u.prefix, u.tok).slots + kTileSlots - 1) / kTileSlots, 1);
+    auto pair = [&](int c) {                             // pair number c, in the order of the rows
+        int lo = 0, hi = B - 1;                          // the first b with base[b + 1] > c
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (x.base[mid + 1] > c) hi = mid; else lo = mid + 1;
         }
+        Unit u;
+        u.b = lo; u.row0 = x.row0[lo]; u.n = x.n[lo]; u.prefix = x.prefix[lo];
+        u.tok = (c - x.base[lo]) * 2 * p.nt;
+        u.layer = u.hs = 0;
+        u.tiles = tiles_of(p, u.n, u.prefix, u.tok);
+        return u;
+    };
+    Unit mine = {};
+    int total = 0, cum = 0;                              // tiles of all pairs; of those before `mine`
+    for (int c0 = 0; c0 < pairs; c0 += kThreads) {
+        mine = {};
+        if (c0 + tid < pairs) mine = pair(c0 + tid);
         int all;
-        const int incl = block_scan(u.tiles, s_warp, &all);
-        u.cum = total + incl - u.tiles;
-        if (c < n_cls) p.classes[c] = u;
+        cum = total + block_scan(mine.tiles, ctrl->scan, &all) - mine.tiles;
         total += all;
     }
-    // (every thread has the same total)
-    const long long seq = (long long)p.c.L * p.n_hs * total;
+    const int lh = p.c.L * p.n_hs;
+    const long long seq = (long long)lh * total, units = (long long)lh * pairs;
     if (seq >= (1ll << 31)) {
-        if (tid == 0) causal::report(p.c.status, MIRROR_DEV_CHECK, 833);
-        n_cls = total = 0;
+        if (tid == 0) {
+            causal::report(p.c.status, MIRROR_DEV_CHECK, 833);
+            p.c.begins[cta] = {0, 0, 0, 0};
+        }
+        return;
     }
-    __syncthreads();                                     // classes[] written by this block are read below
-    if (tid <= p.n_cta) {
-        // boundary tid of n_cta + 1
-        const int used = (int)min((long long)p.n_cta, max(seq, 1ll));
-        CtaStart s = {};
-        long long x = 0;
-        if (total == 0 || tid >= used) {
-            x = total == 0 ? 0 : seq;
-        } else if (tid > 0) {
-            x = seq * tid / used;
-            const long long share = seq / used;
-            const int per = total;                       // tiles of one (layer, head)
-            const long long lh = x / per;
-            int rem = (int)(x - lh * per);
-            int lo = 0, hi = n_cls - 1;                  // the last class with cum <= rem
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (p.classes[mid].cum <= rem) lo = mid; else hi = mid - 1;
+    const int rounds = (int)min((units + p.n_cta - 1) / p.n_cta, 1000ll);
+    auto dealt = [&](int k, int c) -> long long { return (long long)k * p.n_cta + ((k & 1) ? p.n_cta - 1 - c : c); };
+    if (pairs <= kMaxSorted && rounds <= kMaxList) {
+        // longest first; of equals the first
+        if (tid < pairs) x.sorted_tiles[tid] = mine.tiles;
+        __syncthreads();
+        int at = 0;
+        if (tid < pairs)
+            for (int c = 0; c < pairs; ++c) at += x.sorted_tiles[c] > mine.tiles || (x.sorted_tiles[c] == mine.tiles && c < tid);
+        __syncthreads();
+        if (tid < pairs) { x.sorted[at] = tid; x.sorted_tiles[at] = mine.tiles; }
+        __syncthreads();
+        int load = 0;
+        if (tid < p.n_cta)
+            for (int k = 0; k < rounds; ++k) {
+                const long long v = dealt(k, tid);
+                if (v < units) load += x.sorted_tiles[(int)v / lh] + kUnitTiles;
             }
-            const PairClass u = p.classes[lo];
-            s.layer = (int)(lh / p.n_hs);
-            s.hs = (int)(lh - (long long)s.layer * p.n_hs);
-            s.cls = lo;
-            s.t = rem - u.cum;
-            const int tol = (int)min((long long)kSnapTiles, share >> 2);
-            if (s.t <= tol) {
-                x -= s.t;
-                s.t = 0;
-            } else if (u.tiles - s.t <= tol) {
-                x += u.tiles - s.t;
-                s.t = 0;
-                if (++s.cls == n_cls) {
-                    s.cls = 0;
-                    if (++s.hs == p.n_hs) { s.hs = 0; ++s.layer; }
+        load = __reduce_max_sync(0xffffffffu, load);
+        if (lane == 0) atomicMax(&ctrl->makespan, load);
+        __syncthreads();
+        const bool whole = ctrl->makespan <= (int)((seq + units * kUnitTiles) / p.n_cta) + kCutTiles;
+        if (whole) {
+            int tiles = 0;
+            if (tid < rounds) {
+                const long long v = dealt(tid, cta);
+                if (v < units) {
+                    const int r = (int)v / lh, l = (int)v - r * lh;
+                    Unit u = pair(x.sorted[r]);
+                    u.layer = l / p.n_hs;
+                    u.hs = l - u.layer * p.n_hs;
+                    ctrl->list[tid] = u;
+                    tiles = u.tiles;
+                    atomicAdd(&ctrl->n_list, 1);
+                    if (tid == 0) { ctrl->first = u; ctrl->first_t = 0; }
                 }
             }
+            if (tid < 32) {
+                tiles = __reduce_add_sync(0xffffffffu, tiles);
+                if (lane == 0) {
+                    ctrl->n_tiles = tiles;
+                    ctrl->whole = 1;
+                    p.c.begins[cta] = {0, 0, 0, 0};
+                }
+            }
+            return;
         }
-        s_at[tid] = (int)x;
-        if (tid < p.n_cta) {
-            p.starts[tid] = s;
-            p.c.begins[tid] = {x < seq && s.t > 0 ? 1 : 0, s.layer, s.cls, s.hs};
+    }
+    // ---- an even split: where this CTA's range begins and ends
+    const int used = (int)min((long long)p.n_cta, seq);
+    const int tol = (int)min((long long)kSnapTiles, seq / used >> 2);
+    long long x0 = cta >= used ? seq : seq * cta / used, x1 = cta + 1 >= used ? seq : seq * (cta + 1) / used;
+    const int per = total;                               // tiles of one (layer, head)
+    const int lh0 = (int)(x0 / per), rem0 = (int)(x0 - (long long)lh0 * per), rem1 = (int)(x1 % per);
+    int* const s_ends = ctrl->ends;
+    if (tid == 0) { s_ends[0] = (int)x0; s_ends[1] = (int)x1; }
+    int seen = 0;
+    for (int c0 = 0; c0 < pairs; c0 += kThreads) {
+        if (pairs > kThreads) {                          // (a second time: the first kept the last pairs only)
+            mine = {};
+            if (c0 + tid < pairs) mine = pair(c0 + tid);
+            int all;
+            cum = seen + block_scan(mine.tiles, ctrl->scan, &all) - mine.tiles;
+            seen += all;
+        }
+        __syncthreads();
+        if (c0 + tid < pairs) {
+            // (this pair's tiles lie in front of both boundaries' places within their head, or hold them)
+            if (x0 < seq && rem0 >= cum && rem0 < cum + mine.tiles) {
+                Unit u = mine;
+                u.layer = lh0 / p.n_hs;
+                u.hs = lh0 - u.layer * p.n_hs;
+                int t = rem0 - cum;
+                if (cta == 0) t = 0;
+                bool next = false;
+                if (t <= tol) {
+                    s_ends[0] = (int)x0 - t;
+                    t = 0;
+                } else if (mine.tiles - t <= tol) {
+                    s_ends[0] = (int)x0 + mine.tiles - t;
+                    t = 0;
+                    next = true;
+                }
+                ctrl->first = u;
+                ctrl->first_t = next ? -1 : t;
+            }
+            if (x1 < seq && rem1 >= cum && rem1 < cum + mine.tiles) {
+                const int t = rem1 - cum;
+                if (t <= tol) s_ends[1] = (int)x1 - t;
+                else if (mine.tiles - t <= tol) s_ends[1] = (int)x1 + mine.tiles - t;
+            }
         }
     }
     __syncthreads();
-    if (tid < p.n_cta) p.starts[tid].n_tiles = s_at[tid + 1] - s_at[tid];
-    if (tid == 0) p.starts[p.n_cta].cls = n_cls;
-}
-
-// ---- a CTA's way through its units -----------------------------------------------------------------------------
-struct Segment {
-    int layer, hs, cls;
-    int t_first, t_last, tiles;           // tiles [t_first, t_last) of the unit's `tiles`
-    PairClass u;
-    Keys k;
-};
-__device__ __forceinline__ PairClass load_class(const PromptParams& p, int cls) {
-    const int4* src = reinterpret_cast<const int4*>(p.classes + cls);
-    const int4 a = src[0], b = src[1];
-    PairClass u;
-    u.row0 = a.x; u.n = a.y; u.prefix = a.z; u.tok = a.w;
-    u.tiles = b.x; u.cum = b.y; u.b = b.z; u.pad = 0;
-    return u;
-}
-__device__ __forceinline__ void fill_segment(Segment& s, const PromptParams& p, int left) {
-    s.tiles = s.u.tiles;
-    s.t_last = min(s.tiles, s.t_first + left);
-    s.k = pair_keys(p, s.u.n, s.u.prefix, s.u.tok);
-}
-__device__ __noinline__ void next_segment(Segment& s, const PromptParams& p, int n_cls, int left) {
-    if (++s.cls == n_cls) {
-        s.cls = 0;
-        if (++s.hs == p.n_hs) { s.hs = 0; ++s.layer; }
+    if (tid == 0) {
+        const int n = s_ends[1] - s_ends[0];
+        ctrl->n_tiles = n;
+        if (n > 0) {
+            if (ctrl->first_t < 0) {                     // (the boundary moved to the next unit)
+                Segment s;
+                s.u = ctrl->first;
+                s.k = 0;
+                next_segment(s, p, ctrl, n);
+                ctrl->first = s.u;
+                ctrl->first_t = 0;
+            }
+            p.firsts[cta] = ctrl->first;
+            p.c.begins[cta] = {ctrl->first_t > 0 ? 1 : 0, ctrl->first.layer, ctrl->first.row0 + ctrl->first.tok, ctrl->first.hs};
+        } else {
+            p.c.begins[cta] = {0, 0, 0, 0};
+        }
     }
-    s.u = load_class(p, s.cls);
-    s.t_first = 0;
-    fill_segment(s, p, left);
 }
-// Does some row of stream g see something of tile t?  (Its tokens are tok + g nt and the nt - 1 behind it, as far as they exist.)
-struct StreamRows {
-    int first, last;                      // positions; last < first: no rows
-};
-__device__ __forceinline__ StreamRows stream_rows(const PromptParams& p, const Segment& s, int g) {
-    const int t0 = s.u.tok + g * p.nt, t1 = min(t0 + p.nt, s.u.n) - 1;
-    return {s.u.prefix + t0, s.u.prefix + t1};
-}
-__device__ __forceinline__ bool tile_seen(const PromptParams& p, const Segment& s, const StreamRows& r, int t) {
-    const int key0 = s.k.page(t * kTileSlots) * kSlotTok, key1 = s.k.page(min(t * kTileSlots + kTileSlots, s.k.slots) - 1) * kSlotTok + kSlotTok - 1;
-    return r.last >= r.first && key0 <= r.last && (p.c.window == 0 || key1 > r.first - p.c.window || key0 < p.c.n_sink);
-}
-
-struct Ctrl {
-    uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t q_full, q_empty;
-    uint64_t s_full[2], p_full[2][2], o_full[2];        // per stream (P: per half of the tile)
-    uint64_t pv_half[2];
-    uint64_t turn[2];                                   // the issuing warps take turns
-    uint64_t exp_turn[2][4];                            // the two softmax warps of a scheduler take turns
-    CtaStart start;
-    int n_cls;
-    int* status;
-    long long wait_limit;
-    uint32_t tmem_base;
-    volatile int abort;
-};
-static_assert(sizeof(Ctrl) <= kCtrlBytes, "control block");
 
 template <int D>
 struct Cfg {
@@ -274,30 +367,54 @@ struct Cfg {
     static constexpr int kQBytes = kHalves * kQHalfBytes;
 };
 
-// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM.
-__device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, const Keys& k, int pos, int window, int n_sink) {
-#pragma unroll 1
-    for (int c = 0; c < kTileSlots; ++c) {
-        uint32_t m = 0;
-        if (slot0 + c < k.slots) {
-            const int key0 = k.page(slot0 + c) * kSlotTok, at = pos - key0;             // the row's own token, in the slot
-            m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
-            if (window > 0) {
-                const int lo = at - window + 1, sk = n_sink - key0;
-                const uint32_t in = lo <= 0 ? 0xffffu : lo > 15 ? 0u : 0xffffu & ~((1u << lo) - 1u);
-                m &= in | (sk >= 16 ? 0xffffu : sk <= 0 ? 0u : (1u << sk) - 1u);
-            }
+// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM.  Returns the row's maximum where it is asked for.
+__device__ __noinline__ float mask_tile(uint32_t s_addr, int slot0, const Keys& k, int pos, int window, int n_sink, bool want_max) {
+    float mx = -INFINITY;
+    auto bits = [&](int slot) -> uint32_t {
+        if (slot >= k.slots) return 0u;
+        const int key0 = k.page(slot) * kSlotTok, at = pos - key0;                          // the row's own token, in the slot
+        uint32_t m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
+        if (window > 0) {
+            const int lo = at - window + 1, sk = n_sink - key0;
+            const uint32_t in = lo <= 0 ? 0xffffu : lo > 15 ? 0u : 0xffffu & ~((1u << lo) - 1u);
+            m &= in | (sk >= 16 ? 0xffffu : sk <= 0 ? 0u : (1u << sk) - 1u);
         }
-        if (__all_sync(0xffffffffu, m == 0xffffu)) continue;
-        uint32_t r[16];
-        ptx::tmem_ld_32x32b_x16(s_addr + (uint32_t)(c * 16), r);
-        tmem_ld_wait16(r);
+        return m;
+    };
+#pragma unroll 1
+    for (int c = 0; c < kTileSlots / 2; ++c) {
+        const uint32_t m = bits(slot0 + 2 * c) | bits(slot0 + 2 * c + 1) << 16;
+        const bool full = __all_sync(0xffffffffu, m == 0xffffffffu);
+        if (full && !want_max) continue;
+        uint32_t r[32];
+        ptx::tmem_ld_32x32b_x32(s_addr + (uint32_t)(c * 32), r);
+        tmem_ld_wait32(r);
+        if (!full) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (!((m >> j) & 1u)) r[j] = 0xff800000u;
-        tmem_st_32x32b_x16(s_addr + (uint32_t)(c * 16), r);
+            for (int j = 0; j < 32; ++j) r[j] = (m & (1u << j)) ? r[j] : 0xff800000u;
+            tmem_st_32x32b_x32(s_addr + (uint32_t)(c * 32), r);
+        }
+        if (want_max) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(mx) : "f"(__uint_as_float(r[j])), "f"(__uint_as_float(r[j + 1])));
+        }
     }
     tmem_st_wait();
+    return mx;
+}
+
+// 32 bytes of a row
+__device__ __forceinline__ void store32(__nv_bfloat16* dst, const float (&a)[16], bool wide) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = pack_bf16(a[2 * j], a[2 * j + 1]);
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(dst + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
 }
 
 template <int D>
@@ -341,16 +458,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
     ptx::tc_fence_after();
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    if (tid == 0) {
-        ctrl->start = p.starts[blockIdx.x];
-        ctrl->n_cls = p.starts[p.n_cta].cls;                           // (left there by the plan)
-    }
+    make_plan(p, ctrl, (int*)ring);
+    ptx::fence_proxy_async();                            // (the ring is filled by copies from here on)
     __syncthreads();
     const uint32_t tmem_base = ctrl->tmem_base;
-    const int n_tiles = ctrl->start.n_tiles, n_cls = ctrl->n_cls;
+    const int n_tiles = ctrl->n_tiles;
     auto first_segment = [&](Segment& s) {
-        s.layer = ctrl->start.layer; s.hs = ctrl->start.hs; s.cls = ctrl->start.cls; s.t_first = ctrl->start.t;
-        s.u = load_class(p, s.cls);
+        s.u = ctrl->first;
+        s.t_first = ctrl->first_t;
+        s.k = 0;
         fill_segment(s, p, n_tiles);
     };
 
@@ -368,16 +484,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
         int pg = 0, pg_next = 0;
         auto fetch = [&](int tt) -> int {                            // physical pages of a tile, one per lane (0..7)
             const int sl = tt * kTileSlots + lane;
-            return (lane < kTileSlots && sl < sg.k.slots) ? p.c.page_table[(size_t)sg.u.b * p.c.max_pages + sg.k.page(sl)] : 0;
+            return (lane < kTileSlots && sl < sg.keys.slots) ? p.c.page_table[(size_t)sg.u.b * p.c.max_pages + sg.keys.page(sl)] : 0;
         };
         auto load_q = [&]() {
             if (!ptx::warp_wait(ctrl, &ctrl->q_empty, (n_seg & 1) ^ 1, 61)) { ok = false; return; }
             if (ptx::elect_one()) {
-                const int kvh = sg.hs / p.shares, head = kvh * p.c.G + (sg.hs - kvh * p.shares) * p.gs;
+                const int kvh = sg.u.hs / p.shares, head = kvh * p.c.G + (sg.u.hs - kvh * p.shares) * p.gs;
                 ptx::mbar_arrive_expect_tx(&ctrl->q_full, (uint32_t)(2 * C::kHalves * q_rows * 128));
                 for (int g = 0; g < 2; ++g)
                     for (int h = 0; h < C::kHalves; ++h)
-                        ptx::tma_load_5d(sQ + g * C::kQBytes + h * C::kQHalfBytes, &tm.q, &ctrl->q_full, 0, head, sg.layer * p.c.R + sg.u.row0 + sg.u.tok + g * p.nt, h, 0);
+                        ptx::tma_load_5d(sQ + g * C::kQBytes + h * C::kQHalfBytes, &tm.q, &ctrl->q_full, 0, head, sg.u.layer * p.c.R + sg.u.row0 + sg.u.tok + g * p.nt, h, 0);
             }
             __syncwarp();
             ++n_seg;
@@ -400,17 +516,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             if (!ptx::warp_wait(ctrl, &ctrl->empty[st], ((seq / (uint32_t)n_stages) & 1) ^ 1, 60)) { ok = false; break; }
             uint8_t* const dst = ring + (size_t)st * C::kStageBytes;
             uint64_t* const bar = &ctrl->full[st];
-            const int sl0 = t * kTileSlots, n_sl = min(kTileSlots, sg.k.slots - sl0), kvh = sg.hs / p.shares;
+            const int sl0 = t * kTileSlots, n_sl = min(kTileSlots, sg.keys.slots - sl0), kvh = sg.u.hs / p.shares;
             if (pg < 0 || pg >= p.c.num_pages) { causal::report(p.c.status, MIRROR_DEV_CHECK, 832); pg = 0; }
-            const int row0 = sg.layer * p.c.layer_pages;
+            const int row0 = sg.u.layer * p.c.layer_pages;
             uint32_t partial = 0;                                    // V: slots with tokens that no row of the request sees
             if (V) {
-                const int key0 = sg.k.page(sl0 + (lane & 7)) * kSlotTok;
+                const int key0 = sg.keys.page(sl0 + (lane & 7)) * kSlotTok;
                 partial = __ballot_sync(0xffffffffu, lane < n_sl && (key0 + kSlotTok > req_len || (key0 < req_lo && key0 + kSlotTok > req_sink)));
                 if (partial) {
                     for (int k = 0; k < n_sl; ++k) {
                         if (!(partial >> k & 1)) continue;
-                        const int page = __shfl_sync(0xffffffffu, pg, k), base = sg.k.page(sl0 + k) * kSlotTok;
+                        const int page = __shfl_sync(0xffffffffu, pg, k), base = sg.keys.page(sl0 + k) * kSlotTok;
                         const uint8_t* const src = (const uint8_t*)p.c.v_pool + ((size_t)(row0 + page) * p.c.Hkv + kvh) * (size_t)C::kSlotBytes;
                         constexpr int kRowChunks = D / 8;
 #pragma unroll 1
@@ -449,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             seq += 2;
             --left;
             if (++t == sg.t_last && left > 0) {
-                next_segment(sg, p, n_cls, left);
+                next_segment(sg, p, ctrl, left);
                 t = 0;
                 request();
                 pg_next = fetch(0);
@@ -522,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             if (!ok) break;
             ptx::tc_fence_after();
             const bool qk_on = has_qk && tile_seen(p, sg, rows, t), qk_last = has_qk && t + 1 == sg.t_last;
-            const int qk_sl = has_qk ? min(kTileSlots, sg.k.slots - t * kTileSlots) : 0;
+            const int qk_sl = has_qk ? min(kTileSlots, sg.keys.slots - t * kTileSlots) : 0;
             const uint32_t idesc_qk = ptx::umma_idesc_bf16(kRows, qk_sl * kSlotTok), kb = k_lo + kst * (uint32_t)(C::kStageBytes >> 4);
             if (ptx::elect_one()) {
                 if (has_pv) {
@@ -551,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             pv_sl = qk_sl;
             --left;
             if (++t == sg.t_last && left > 0) {
-                next_segment(sg, p, n_cls, left);
+                next_segment(sg, p, ctrl, left);
                 rows = stream_rows(p, sg, g);
                 t = 0;
             }
@@ -582,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
 #pragma unroll 1
         while (left > 0 && ok) {
             const StreamRows rows = stream_rows(p, sg, grp);
-            const int kvh = sg.hs / p.shares, hg = (sg.hs - kvh * p.shares) * p.gs + hl;                     // head within the group
+            const int kvh = sg.u.hs / p.shares, hg = (sg.u.hs - kvh * p.shares) * p.gs + hl;                     // head within the group
             const int tok = sg.u.tok + grp * p.nt + it, pos = sg.u.prefix + tok;
             const bool row_ok = it < p.nt && tok < sg.u.n && hg < p.c.G;
             const bool warp_has_rows = __any_sync(0xffffffffu, row_ok);
@@ -595,13 +711,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                 s_par ^= 1;
                 ptx::tc_fence_after();
                 if (warp_has_rows && on) {
-                    const int key0 = sg.k.page(t * kTileSlots) * kSlotTok;
-                    const bool whole_tile = (t + 1) * kTileSlots <= sg.k.slots && sg.k.page(t * kTileSlots + kTileSlots - 1) * kSlotTok + kSlotTok - 1 <= rows.first &&
+                    const int key0 = sg.keys.page(t * kTileSlots) * kSlotTok;
+                    const bool whole_tile = (t + 1) * kTileSlots <= sg.keys.slots && sg.keys.page(t * kTileSlots + kTileSlots - 1) * kSlotTok + kSlotTok - 1 <= rows.first &&
                                             (p.c.window == 0 || key0 > rows.last - p.c.window);
-                    if (!whole_tile) mask_tile(s_addr, t * kTileSlots, sg.k, pos, p.c.window, p.c.n_sink);
-                    if (__any_sync(0xffffffffu, off == -INFINITY)) {
-                        const float mx = tile_max(s_addr, 4);
-                        if (off == -INFINITY) off = mx * sc;
+                    // The offset is set by the first tile in which the row sees anything (before that every P was 0).
+                    const bool set_off = __any_sync(0xffffffffu, off == -INFINITY);
+                    if (!whole_tile || set_off) {
+                        const float mx = whole_tile ? tile_max(s_addr, 4) : mask_tile(s_addr, t * kTileSlots, sg.keys, pos, p.c.window, p.c.n_sink, set_off);
+                        if (off == -INFINITY) off = mx * sc;       // (-inf when nothing is visible yet)
                     }
                     float sum = 0.f;
                     uint32_t ra[32];
@@ -659,8 +776,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             }
             if (!ok) break;
             // ---- end of this CTA's part of the unit
-            const bool whole = sg.t_first == 0 && sg.t_last == sg.tiles;
-            const size_t at = ((size_t)sg.layer * p.c.R + sg.u.row0 + tok) * p.c.Hq + kvh * p.c.G + hg;
+            const bool whole = sg.t_first == 0 && sg.t_last == sg.u.tiles;
+            const size_t at = ((size_t)sg.u.layer * p.c.R + sg.u.row0 + tok) * p.c.Hq + kvh * p.c.G + hg;
             __nv_bfloat16* const orow = p.c.out + at * D;
             const int slot = sg.t_first > 0 ? 0 : 1;                 // a unit that began before this CTA's range uses slot 0
             float* const rec = p.c.partial + (((size_t)blockIdx.x * 2 + slot) * 2 + grp) * kRowW * kRows + row;
@@ -684,8 +801,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
 #pragma unroll
                         for (int j = 0; j < 16; ++j) rec[(size_t)(c + j) * kRows] = acc[j];
                     } else if (row_ok) {
-                        *reinterpret_cast<uint4*>(orow + c) = make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
-                        *reinterpret_cast<uint4*>(orow + c + 8) = make_uint4(pack_bf16(acc[8], acc[9]), pack_bf16(acc[10], acc[11]), pack_bf16(acc[12], acc[13]), pack_bf16(acc[14], acc[15]));
+                        store32(orow + c, acc, p.wide_out != 0);
                     }
                 }
                 if (!whole) {
@@ -697,7 +813,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             }
             // (the stream's next P V waits for a P that its own warps write after this)
             ptx::tc_fence_before();
-            if (left > 0) next_segment(sg, p, n_cls, left);
+            if (left > 0) next_segment(sg, p, ctrl, left);
         }
     }
 
@@ -718,7 +834,7 @@ __global__ void __launch_bounds__(kMergeThreads) attn_prompt_merge_kernel(const 
     merge_boundary<D>(
         p.c.begins, p.n_cta, p.c.out, p.c.lse_out, p.c.status, p.c.wait_limit, 0,
         [&](int row, const GroupBegin& u, size_t& place, size_t& lse_place) {
-            const PairClass c = load_class(p, u.b);
+            const Unit c = p.firsts[blockIdx.x + 1];                 // (the boundary's unit)
             const int it = row / p.gs, hl = row - it * p.gs, kvh = u.g / p.shares, hg = (u.g - kvh * p.shares) * p.gs + hl, tok = c.tok + grp * p.nt + it;
             place = lse_place = ((size_t)u.layer * p.c.R + c.row0 + tok) * p.c.Hq + kvh * p.c.G + hg;
             return it < p.nt && tok < c.n && hg < p.c.G;
@@ -732,17 +848,11 @@ void row_tile(int G, int* gs, int* shares, int* nt) {
     *gs = (G + *shares - 1) / *shares;
     *nt = kRows / *gs;
 }
-int most_classes(const mirror_ctx* ctx, int n_rows, int batch) {
-    int gs, shares, nt;
-    row_tile(ctx->desc.n_q_heads / ctx->desc.n_kv_heads, &gs, &shares, &nt);
-    return n_rows / (2 * nt) + batch + 1;
-}
-
 }  // namespace
 
 size_t mirror_attn_prompt_plan_bytes(const mirror_ctx* ctx, const mirror_rows* rows) {
-    return align_up(((size_t)ctx->num_sms + 1) * sizeof(CtaStart), 256) +
-           align_up((size_t)most_classes(ctx, rows->n_rows, rows->batch) * sizeof(PairClass), 256);
+    (void)rows;
+    return align_up((size_t)ctx->num_sms * sizeof(Unit), 256);
 }
 
 mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& cp, void* plan, cudaStream_t stream) {
@@ -752,10 +862,9 @@ mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, co
     row_tile(cp.G, &p.gs, &p.shares, &p.nt);
     p.n_hs = cp.Hkv * p.shares;
     p.n_cta = ctx->num_sms;
-    p.max_classes = most_classes(ctx, cp.R, cp.B);
-    p.starts = (CtaStart*)plan;
-    p.classes = (PairClass*)((uint8_t*)plan + align_up(((size_t)ctx->num_sms + 1) * sizeof(CtaStart), 256));
-    if (p.n_cta + 1 > kPlanThreads || p.n_cta > 512 || (size_t)p.n_cta * sizeof(GroupBegin) > kWsNotesBytes) return MIRROR_ERR_SHAPE;
+    p.firsts = (Unit*)plan;
+    p.wide_out = ((uintptr_t)cp.out & 31) == 0;
+    if (p.n_cta > kThreads || (size_t)p.n_cta * sizeof(GroupBegin) > kWsNotesBytes) return MIRROR_ERR_SHAPE;
     if ((int64_t)cp.L * cp.R > 0x7fffffff) return MIRROR_ERR_SHAPE;
     Maps tm;
     mirror_status st = mirror_attn_pool_tmap(ctx, kv, kv->k_pool, &tm.k);
@@ -770,7 +879,6 @@ mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, co
         st = mirror_make_tmap(ctx, &tm.q, cp.q, 5, dims, strides, box);
         if (st != MIRROR_OK) return st;
     }
-    MIRROR_CUDA_OK(mirror_launch_pdl(attn_prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p));
     auto launch = [&](auto cfg, auto kern, auto merge) -> mirror_status {
         using C = decltype(cfg);
         const size_t fixed = 2 * (size_t)C::kQBytes + kCtrlBytes;
@@ -783,7 +891,7 @@ mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, co
     };
     st = D == 128 ? launch(Cfg<128>{}, attn_prompt_kernel<128>, attn_prompt_merge_kernel<128>) : launch(Cfg<64>{}, attn_prompt_kernel<64>, attn_prompt_merge_kernel<64>);
     if (st != MIRROR_OK) return st;
-    ctx->launches += 3;
+    ctx->launches += 2;
     MIRROR_CUDA_OK(cudaGetLastError());
     return MIRROR_OK;
 }
