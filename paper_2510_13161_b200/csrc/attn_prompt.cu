@@ -113,9 +113,16 @@ __device__ __forceinline__ bool tile_seen(const PromptParams& p, const Segment& 
     return r.last >= r.first && key0 <= r.last && (p.c.window == 0 || key1 > r.first - p.c.window || key0 < p.c.n_sink);
 }
 
+// ... and of how many of the tile's slots, from its first?  (What lies behind the stream's last row is not multiplied.)
+__device__ __forceinline__ int slots_seen(const Segment& s, const StreamRows& r, int t) {
+    const int most = min(kTileSlots, s.keys.slots - t * kTileSlots), page0 = s.keys.page(t * kTileSlots);
+    const int jump = s.keys.sink_slots > t * kTileSlots ? s.keys.from - s.keys.sink_slots : 0;         // (sinks and window in one tile: by its last slot)
+    return max(1, min(most, r.last / kSlotTok + 1 - page0 + (jump > 0 ? most : 0)));
+}
+
 struct Ctrl {
     uint64_t full[kMaxStages], empty[kMaxStages];
-    uint64_t q_full, q_empty;
+    uint64_t q_full[2], q_empty[2];                     // per stream: one is through with a unit long before the other
     uint64_t s_full[2], p_full[2][2], o_full[2];        // per stream (P: per half of the tile)
     uint64_t pv_half[2];
     uint64_t turn[2];                                   // the issuing warps take turns
@@ -244,23 +251,26 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
         return;
     }
     const int rounds = (int)min((units + p.n_cta - 1) / p.n_cta, 1000ll);
-    auto dealt = [&](int k, int c) -> long long { return (long long)k * p.n_cta + ((k & 1) ? p.n_cta - 1 - c : c); };
+    auto dealt = [&](int k, int c) -> int { return k * p.n_cta + ((k & 1) ? p.n_cta - 1 - c : c); };          // (few rounds)
     if (pairs <= kMaxSorted && rounds <= kMaxList) {
         // longest first; of equals the first
         if (tid < pairs) x.sorted_tiles[tid] = mine.tiles;
         __syncthreads();
         int at = 0;
         if (tid < pairs)
+#pragma unroll 8
             for (int c = 0; c < pairs; ++c) at += x.sorted_tiles[c] > mine.tiles || (x.sorted_tiles[c] == mine.tiles && c < tid);
         __syncthreads();
         if (tid < pairs) { x.sorted[at] = tid; x.sorted_tiles[at] = mine.tiles; }
         __syncthreads();
         int load = 0;
-        if (tid < p.n_cta)
+        if (tid < p.n_cta) {
+#pragma unroll 4
             for (int k = 0; k < rounds; ++k) {
-                const long long v = dealt(k, tid);
-                if (v < units) load += x.sorted_tiles[(int)v / lh] + kUnitTiles;
+                const uint32_t v = (uint32_t)dealt(k, tid);
+                if (v < (uint32_t)units) load += x.sorted_tiles[v / (uint32_t)lh] + kUnitTiles;
             }
+        }
         load = __reduce_max_sync(0xffffffffu, load);
         if (lane == 0) atomicMax(&ctrl->makespan, load);
         __syncthreads();
@@ -268,9 +278,9 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
         if (whole) {
             int tiles = 0;
             if (tid < rounds) {
-                const long long v = dealt(tid, cta);
+                const int v = dealt(tid, cta);
                 if (v < units) {
-                    const int r = (int)v / lh, l = (int)v - r * lh;
+                    const int r = v / lh, l = v - r * lh;
                     Unit u = pair(x.sorted[r]);
                     u.layer = l / p.n_hs;
                     u.hs = l - u.layer * p.n_hs;
@@ -367,8 +377,9 @@ struct Cfg {
     static constexpr int kQBytes = kHalves * kQHalfBytes;
 };
 
-// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM.  Returns the row's maximum where it is asked for.
-__device__ __noinline__ float mask_tile(uint32_t s_addr, int slot0, const Keys& k, int pos, int window, int n_sink, bool want_max) {
+// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM; `rows` are the stream's positions.  Returns the row's
+// maximum where it is asked for.  (Two slots at a time: most of a tile's pairs are seen by all rows, or by none.)
+__device__ __noinline__ float mask_tile(uint32_t s_addr, int slot0, const Keys& k, int pos, const StreamRows& rows, int window, int n_sink, int chunks, bool want_max) {
     float mx = -INFINITY;
     auto bits = [&](int slot) -> uint32_t {
         if (slot >= k.slots) return 0u;
@@ -382,17 +393,26 @@ __device__ __noinline__ float mask_tile(uint32_t s_addr, int slot0, const Keys& 
         return m;
     };
 #pragma unroll 1
-    for (int c = 0; c < kTileSlots / 2; ++c) {
-        const uint32_t m = bits(slot0 + 2 * c) | bits(slot0 + 2 * c + 1) << 16;
-        const bool full = __all_sync(0xffffffffu, m == 0xffffffffu);
-        if (full && !want_max) continue;
+    for (int c = 0; c < chunks; ++c, s_addr += 32) {
+        const int a = slot0 + 2 * c;
         uint32_t r[32];
-        ptx::tmem_ld_32x32b_x32(s_addr + (uint32_t)(c * 32), r);
+        const int key0 = k.page(a) * kSlotTok, key1 = k.page(min(a + 1, k.slots - 1)) * kSlotTok + kSlotTok - 1;
+        const bool none = a >= k.slots || key0 > rows.last || (window > 0 && key1 <= rows.first - window && key0 >= n_sink);
+        if (none) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = 0xff800000u;
+            tmem_st_32x32b_x32(s_addr, r);
+            continue;
+        }
+        const bool all = a + 1 < k.slots && key1 <= rows.first && (window == 0 || key0 > rows.last - window || key1 < n_sink);
+        if (all && !want_max) continue;
+        ptx::tmem_ld_32x32b_x32(s_addr, r);
+        const uint32_t m = all ? 0xffffffffu : bits(a) | bits(a + 1) << 16;
         tmem_ld_wait32(r);
-        if (!full) {
+        if (!all) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) r[j] = (m & (1u << j)) ? r[j] : 0xff800000u;
-            tmem_st_32x32b_x32(s_addr + (uint32_t)(c * 32), r);
+            tmem_st_32x32b_x32(s_addr, r);
         }
         if (want_max) {
 #pragma unroll
@@ -404,10 +424,10 @@ __device__ __noinline__ float mask_tile(uint32_t s_addr, int slot0, const Keys& 
 }
 
 // 32 bytes of a row
-__device__ __forceinline__ void store32(__nv_bfloat16* dst, const float (&a)[16], bool wide) {
+__device__ __forceinline__ void store32(__nv_bfloat16* dst, const uint32_t* a, float f, bool wide) {
     uint32_t w[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = pack_bf16(a[2 * j], a[2 * j + 1]);
+    for (int j = 0; j < 8; ++j) w[j] = pack_bf16(f * __uint_as_float(a[2 * j]), f * __uint_as_float(a[2 * j + 1]));
     if (wide) {
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                      ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
@@ -429,9 +449,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
     // ---- prologue, while the kernel ahead is still running: nothing of global memory is touched
     if (tid == 0) {
         for (int s = 0; s < n_stages; ++s) { ptx::mbar_init(&ctrl->full[s], 1); ptx::mbar_init(&ctrl->empty[s], 2); }
-        ptx::mbar_init(&ctrl->q_full, 1);
-        ptx::mbar_init(&ctrl->q_empty, 2);
         for (int g = 0; g < 2; ++g) {
+            ptx::mbar_init(&ctrl->q_full[g], 1); ptx::mbar_init(&ctrl->q_empty[g], 1);
             ptx::mbar_init(&ctrl->s_full[g], 1); ptx::mbar_init(&ctrl->p_full[g][0], 4); ptx::mbar_init(&ctrl->p_full[g][1], 4);
             ptx::mbar_init(&ctrl->o_full[g], 1); ptx::mbar_init(&ctrl->turn[g], 1); ptx::mbar_init(&ctrl->pv_half[g], 1);
             for (int s = 0; s < 4; ++s) ptx::mbar_init(&ctrl->exp_turn[g][s], 1);
@@ -487,15 +506,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             return (lane < kTileSlots && sl < sg.keys.slots) ? p.c.page_table[(size_t)sg.u.b * p.c.max_pages + sg.keys.page(sl)] : 0;
         };
         auto load_q = [&]() {
-            if (!ptx::warp_wait(ctrl, &ctrl->q_empty, (n_seg & 1) ^ 1, 61)) { ok = false; return; }
-            if (ptx::elect_one()) {
-                const int kvh = sg.u.hs / p.shares, head = kvh * p.c.G + (sg.u.hs - kvh * p.shares) * p.gs;
-                ptx::mbar_arrive_expect_tx(&ctrl->q_full, (uint32_t)(2 * C::kHalves * q_rows * 128));
-                for (int g = 0; g < 2; ++g)
+            const int kvh = sg.u.hs / p.shares, head = kvh * p.c.G + (sg.u.hs - kvh * p.shares) * p.gs;
+            for (int g = 0; g < 2; ++g) {
+                if (!ptx::warp_wait(ctrl, &ctrl->q_empty[g], (n_seg & 1) ^ 1, 61)) { ok = false; return; }
+                if (ptx::elect_one()) {
+                    ptx::mbar_arrive_expect_tx(&ctrl->q_full[g], (uint32_t)(C::kHalves * q_rows * 128));
                     for (int h = 0; h < C::kHalves; ++h)
-                        ptx::tma_load_5d(sQ + g * C::kQBytes + h * C::kQHalfBytes, &tm.q, &ctrl->q_full, 0, head, sg.u.layer * p.c.R + sg.u.row0 + sg.u.tok + g * p.nt, h, 0);
+                        ptx::tma_load_5d(sQ + g * C::kQBytes + h * C::kQHalfBytes, &tm.q, &ctrl->q_full[g], 0, head, sg.u.layer * p.c.R + sg.u.row0 + sg.u.tok + g * p.nt, h, 0);
+                }
+                __syncwarp();
             }
-            __syncwarp();
             ++n_seg;
         };
         // what some row of the request sees (see causal::Request); the rest of V may be anything, and is taken as zeros
@@ -578,7 +598,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                 seq -= 2;
                 ptx::mbar_wait(&ctrl->full[seq % (uint32_t)n_stages], (seq / (uint32_t)n_stages) & 1, 20000000ll);
             }
-            if (V && n_seg > 0) ptx::mbar_wait(&ctrl->q_full, (n_seg - 1) & 1, 20000000ll);
+            // (of a unit whose second Q was not asked for the wait runs out: it is bounded)
+            if (V && n_seg > 0)
+                for (int g = 0; g < 2; ++g) ptx::mbar_wait(&ctrl->q_full[g], (n_seg - 1) & 1, 20000000ll);
         }
     } else if (warp < 4) {
         // ======================================================================= tensor-core issuers (see attn_verify.cu)
@@ -613,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             if (has_pv) vst = take();
             if (has_qk) {
                 kst = take();
-                if (t == sg.t_first) { wait(&ctrl->q_full, q_par, 63); q_par ^= 1; }
+                if (t == sg.t_first) { wait(&ctrl->q_full[g], q_par, 63); q_par ^= 1; }
             }
             const uint32_t vb = v_lo + vst * (uint32_t)(C::kStageBytes >> 4);
             auto pv = [&](int k0, int k1) {
@@ -638,7 +660,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             if (!ok) break;
             ptx::tc_fence_after();
             const bool qk_on = has_qk && tile_seen(p, sg, rows, t), qk_last = has_qk && t + 1 == sg.t_last;
-            const int qk_sl = has_qk ? min(kTileSlots, sg.keys.slots - t * kTileSlots) : 0;
+            const int qk_sl = has_qk ? slots_seen(sg, rows, t) : 0;
             const uint32_t idesc_qk = ptx::umma_idesc_bf16(kRows, qk_sl * kSlotTok), kb = k_lo + kst * (uint32_t)(C::kStageBytes >> 4);
             if (ptx::elect_one()) {
                 if (has_pv) {
@@ -654,7 +676,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                     }
                     ptx::umma_commit(&ctrl->s_full[g]);
                     ptx::umma_commit(&ctrl->empty[kst]);
-                    if (qk_last) ptx::umma_commit(&ctrl->q_empty);
+                    if (qk_last) ptx::umma_commit(&ctrl->q_empty[g]);
                 }
                 ptx::mbar_arrive(&ctrl->turn[g ^ 1]);
             }
@@ -714,10 +736,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                     const int key0 = sg.keys.page(t * kTileSlots) * kSlotTok;
                     const bool whole_tile = (t + 1) * kTileSlots <= sg.keys.slots && sg.keys.page(t * kTileSlots + kTileSlots - 1) * kSlotTok + kSlotTok - 1 <= rows.first &&
                                             (p.c.window == 0 || key0 > rows.last - p.c.window);
+                    // Two halves of 64 scores, one copy of the code (the second left out where no row sees it).  P of a half goes over S columns
+                    // that have been read.
+                    const int halves = slots_seen(sg, rows, t) > kTileSlots / 2 ? 2 : 1;
                     // The offset is set by the first tile in which the row sees anything (before that every P was 0).
                     const bool set_off = __any_sync(0xffffffffu, off == -INFINITY);
                     if (!whole_tile || set_off) {
-                        const float mx = whole_tile ? tile_max(s_addr, 4) : mask_tile(s_addr, t * kTileSlots, sg.keys, pos, p.c.window, p.c.n_sink, set_off);
+                        const float mx = whole_tile ? tile_max(s_addr, 4) : mask_tile(s_addr, t * kTileSlots, sg.keys, pos, rows, p.c.window, p.c.n_sink, 2 * halves, set_off);
                         if (off == -INFINITY) off = mx * sc;       // (-inf when nothing is visible yet)
                     }
                     float sum = 0.f;
@@ -725,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                     ptx::tmem_ld_32x32b_x32(s_addr, ra);
                     if (!take_turn()) { ok = false; break; }
 #pragma unroll 1
-                    for (int h = 0; h < 2;) {
+                    for (int h = 0; h < halves;) {
                         uint32_t pk[32], rb[32];
                         const float o = (off == -INFINITY) ? 0.f : -off;
                         const uint64_t no2 = pack2(o, o);
@@ -735,11 +760,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                         exp_chunk<false>(ra, sc2, no2, pk, s0, s1);
                         tmem_ld_wait32(rb);
                         ptx::tmem_ld_32x32b_x32(s_addr + 64, ra);    // (of no use to the second half)
+                        if (h == halves - 1 && !redone) pass_turn();
                         exp_chunk<false>(rb, sc2, no2, pk + 16, s0, s1);
                         float a, b;
                         unpack2(add2(s0, s1), a, b);
                         const float half_sum = a + b;
-                        if (h == 1 && !redone) pass_turn();
                         const bool grow = half_sum > kSumLimit && !redone;
                         if (__any_sync(0xffffffffu, grow)) {
                             tmem_ld_wait32(ra);
@@ -766,6 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                     }
                     if (!ok) break;
                     tmem_ld_wait32(ra);
+                    if (halves == 1 && lane == 0) ptx::mbar_arrive(&ctrl->p_full[grp][1]);
                     l_run += sum;
                 } else {
                     if (!take_turn()) { ok = false; break; }
@@ -789,19 +815,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                 const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
                 const float w = off == -INFINITY || !any_tile ? 0.f : whole ? inv : 1.f;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    uint32_t r[16];
-                    float acc[16];
-                    ptx::tmem_ld_32x32b_x16(o_addr + (uint32_t)c, r);
-                    tmem_ld_wait16(r);
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t r[32];
+                    ptx::tmem_ld_32x32b_x32(o_addr + (uint32_t)c, r);
+                    tmem_ld_wait32(r);
                     // (an accumulator that no P V wrote may hold anything: a weight of 0 does not read it)
+                    if (w == 0.f) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[j] = w != 0.f ? w * __uint_as_float(r[j]) : 0.f;
+                        for (int j = 0; j < 32; ++j) r[j] = 0u;
+                    }
                     if (!whole) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) rec[(size_t)(c + j) * kRows] = acc[j];
+                        for (int j = 0; j < 32; ++j) rec[(size_t)(c + j) * kRows] = __uint_as_float(r[j]);
                     } else if (row_ok) {
-                        store32(orow + c, acc, p.wide_out != 0);
+                        store32(orow + c, r, w, p.wide_out != 0);
+                        store32(orow + c + 16, r + 16, w, p.wide_out != 0);
                     }
                 }
                 if (!whole) {
