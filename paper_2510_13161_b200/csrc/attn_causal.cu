@@ -458,7 +458,7 @@ mirror_status token_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalPar
     if (st == MIRROR_OK) st = mirror_attn_pool_tmap(ctx, kv, kv->v_pool, &tm.v);
     if (st != MIRROR_OK) return st;
     // Units of at most 32 slots take a CTA less time whole (8 slots a warp) than a launch that merges their parts.
-    const int never_cut = causal_most_slots(p) <= 32;
+    const int never_cut = causal_most_slots(p, p.max_rows) <= 32;
     const int ctas = 2 * ctx->num_sms;
     static_assert(sizeof(attn::GroupBegin) == 16, "notes");
     if (ctas > 1024 || (size_t)ctas * sizeof(attn::GroupBegin) > kWsNotesBytes) return MIRROR_ERR_SHAPE;

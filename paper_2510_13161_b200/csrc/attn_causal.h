@@ -21,10 +21,10 @@ struct CausalParams {
 };
 
 // How long a request can be, as far as the host knows: 16-token slots that its rows see.
-static inline long long causal_most_slots(const CausalParams& p) {
+static inline long long causal_most_slots(const CausalParams& p, int rows) {       // of `rows` neighbouring rows
     long long s = p.max_pages;
     if (p.window > 0) {
-        const long long w = ((long long)p.window + p.max_rows + 14) / 16 + 1 + ((long long)p.n_sink + 15) / 16;
+        const long long w = ((long long)p.window + rows + 14) / 16 + 1 + ((long long)p.n_sink + 15) / 16;
         if (w < s) s = w;
     }
     return s;

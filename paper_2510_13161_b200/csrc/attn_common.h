@@ -69,7 +69,8 @@ struct GroupBegin {
 };
 constexpr int kMergeThreads = 512;        // 128 rows x 4 column quarters
 constexpr int kMergeSlots = 32;           // (part, 8-column chunk) pairs in shared memory at a time
-constexpr int kMergeSmem = kMergeSlots * 10 * 128 * 4;      // their columns, then the parts' (max, sum)
+constexpr int merge_smem(int slots) { return slots * 10 * 128 * 4; }      // their columns, then the parts' (max, sum)
+constexpr int kMergeSmem = merge_smem(kMergeSlots);
 
 // A block per (inner boundary, row tile).  A unit cut by k boundaries left k + 1 (max, sum, accumulator) records, like
 // split-KV partials; the k blocks of those boundaries share its merge by output columns (8-column chunks dealt
@@ -83,7 +84,7 @@ constexpr int kMergeSmem = kMergeSlots * 10 * 128 * 4;      // their columns, th
 // map(row, GroupBegin) -> false, or the places of the row's output (in rows of D) and of its lse; record(group, slot) -> its record in slot 0 (of the unit
 // that began before the group's range) or 1, [column][128 rows], D accumulator columns, then (max, sum).  wait_limit: SM cycles
 // after which a wait gives up; stall: test aid, 1 makes the first wait run out (it expects bytes that nobody copies).
-template <int D, class Map, class Record>
+template <int D, int kMergeSlots = attn::kMergeSlots, class Map, class Record>
 __device__ __forceinline__ void merge_boundary(const GroupBegin* table, int n_groups, __nv_bfloat16* out, float* lse_out, int* status, long long wait_limit, int stall, Map map, Record record) {
     extern __shared__ __align__(128) float s_cols[];                            // [slot][8 columns][128 rows]
     float(*const s_ml)[2][128] = (float(*)[2][128])(s_cols + kMergeSlots * 8 * 128);     // [part][max, then weight | sum][128 rows]

@@ -46,6 +46,7 @@ constexpr int kUnitTiles = 1;                       // what a unit costs beside 
 constexpr int kCutTiles = 6;                        // what cutting costs: a record, a unit more, the merge behind
 constexpr int kMaxList = 24;                        // whole units of a CTA
 constexpr int kMaxSorted = kThreads;                // pairs that are sorted
+constexpr int kMergeSlotsPrompt = 8;                // (most calls have nothing to merge, or two parts: small blocks, all resident at once)
 
 // A unit: a pair of row tiles of one request, of one layer and head.
 struct Unit {
@@ -62,6 +63,7 @@ struct PromptParams {
     int n_hs;                             // KV heads x shares
     int n_cta;
     int wide_out;                         // out on a 32-byte boundary
+    int never_cut;                        // units are dealt out whole whatever their lengths: no merge is launched
     Unit* firsts;                         // [n_cta] the unit that each CTA's range begins in, for the merge
 };
 
@@ -253,28 +255,42 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
     const int rounds = (int)min((units + p.n_cta - 1) / p.n_cta, 1000ll);
     auto dealt = [&](int k, int c) -> int { return k * p.n_cta + ((k & 1) ? p.n_cta - 1 - c : c); };          // (few rounds)
     if (pairs <= kMaxSorted && rounds <= kMaxList) {
-        // longest first; of equals the first
-        if (tid < pairs) x.sorted_tiles[tid] = mine.tiles;
-        __syncthreads();
-        int at = 0;
-        if (tid < pairs)
+        if (tid < pairs) {
+            x.sorted[tid] = tid;
+            x.sorted_tiles[tid] = mine.tiles;
+        }
+        bool whole = p.never_cut != 0;
+        if (rounds == 1) {                               // (nothing to sort: a CTA has one unit at most)
+            if (!whole) {
+                const int load = __reduce_max_sync(0xffffffffu, mine.tiles + kUnitTiles);
+                if (lane == 0) atomicMax(&ctrl->makespan, load);
+            }
+            __syncthreads();
+        } else {
+            // longest first; of equals the first
+            __syncthreads();
+            int at = 0;
+            if (tid < pairs)
 #pragma unroll 8
-            for (int c = 0; c < pairs; ++c) at += x.sorted_tiles[c] > mine.tiles || (x.sorted_tiles[c] == mine.tiles && c < tid);
-        __syncthreads();
-        if (tid < pairs) { x.sorted[at] = tid; x.sorted_tiles[at] = mine.tiles; }
-        __syncthreads();
-        int load = 0;
-        if (tid < p.n_cta) {
+                for (int c = 0; c < pairs; ++c) at += x.sorted_tiles[c] > mine.tiles || (x.sorted_tiles[c] == mine.tiles && c < tid);
+            __syncthreads();
+            if (tid < pairs) { x.sorted[at] = tid; x.sorted_tiles[at] = mine.tiles; }
+            __syncthreads();
+            if (!whole) {
+                int load = 0;
+                if (tid < p.n_cta) {
 #pragma unroll 4
-            for (int k = 0; k < rounds; ++k) {
-                const uint32_t v = (uint32_t)dealt(k, tid);
-                if (v < (uint32_t)units) load += x.sorted_tiles[v / (uint32_t)lh] + kUnitTiles;
+                    for (int k = 0; k < rounds; ++k) {
+                        const uint32_t v = (uint32_t)dealt(k, tid);
+                        if (v < (uint32_t)units) load += x.sorted_tiles[v / (uint32_t)lh] + kUnitTiles;
+                    }
+                }
+                load = __reduce_max_sync(0xffffffffu, load);
+                if (lane == 0) atomicMax(&ctrl->makespan, load);
+                __syncthreads();
             }
         }
-        load = __reduce_max_sync(0xffffffffu, load);
-        if (lane == 0) atomicMax(&ctrl->makespan, load);
-        __syncthreads();
-        const bool whole = ctrl->makespan <= (int)((seq + units * kUnitTiles) / p.n_cta) + kCutTiles;
+        whole |= ctrl->makespan <= (int)((seq + units * kUnitTiles) / p.n_cta) + kCutTiles;
         if (whole) {
             int tiles = 0;
             if (tid < rounds) {
@@ -859,7 +875,7 @@ __global__ void __launch_bounds__(kMergeThreads) attn_prompt_merge_kernel(const 
     const int grp = blockIdx.y;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    merge_boundary<D>(
+    merge_boundary<D, kMergeSlotsPrompt>(
         p.c.begins, p.n_cta, p.c.out, p.c.lse_out, p.c.status, p.c.wait_limit, 0,
         [&](int row, const GroupBegin& u, size_t& place, size_t& lse_place) {
             const Unit c = p.firsts[blockIdx.x + 1];                 // (the boundary's unit)
@@ -892,6 +908,9 @@ mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, co
     p.n_cta = ctx->num_sms;
     p.firsts = (Unit*)plan;
     p.wide_out = ((uintptr_t)cp.out & 31) == 0;
+    // No unit is cut where even the longest that the page table allows is over before a cut would pay (and the CTAs' lists hold them all).
+    const int64_t pairs = cp.R / (2 * p.nt) + cp.B, most_tiles = (causal_most_slots(cp, 2 * p.nt) + kTileSlots - 1) / kTileSlots;
+    p.never_cut = most_tiles <= kCutTiles && pairs <= kMaxSorted && (pairs * cp.L * p.n_hs + ctx->num_sms - 1) / ctx->num_sms <= kMaxList;
     if (p.n_cta > kThreads || (size_t)p.n_cta * sizeof(GroupBegin) > kWsNotesBytes) return MIRROR_ERR_SHAPE;
     if ((int64_t)cp.L * cp.R > 0x7fffffff) return MIRROR_ERR_SHAPE;
     Maps tm;
@@ -913,13 +932,16 @@ mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, co
         const int stages = std::min((int)((kSmemLimit - fixed) / C::kStageBytes), kMaxStages);
         MIRROR_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit));
         MIRROR_CUDA_OK(mirror_launch_pdl(kern, dim3((unsigned)p.n_cta), dim3(kThreads), fixed + (size_t)stages * C::kStageBytes, stream, tm, p, stages));
-        MIRROR_CUDA_OK(cudaFuncSetAttribute(merge, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmem));
-        MIRROR_CUDA_OK(mirror_launch_pdl(merge, dim3((unsigned)(p.n_cta - 1), 2), dim3(kMergeThreads), kMergeSmem, stream, p));
+        ctx->launches += 1;
+        if (p.never_cut) return MIRROR_OK;
+        constexpr int kSmem = merge_smem(kMergeSlotsPrompt);
+        MIRROR_CUDA_OK(cudaFuncSetAttribute(merge, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        MIRROR_CUDA_OK(mirror_launch_pdl(merge, dim3((unsigned)(p.n_cta - 1), 2), dim3(kMergeThreads), kSmem, stream, p));
+        ctx->launches += 1;
         return MIRROR_OK;
     };
     st = D == 128 ? launch(Cfg<128>{}, attn_prompt_kernel<128>, attn_prompt_merge_kernel<128>) : launch(Cfg<64>{}, attn_prompt_kernel<64>, attn_prompt_merge_kernel<64>);
     if (st != MIRROR_OK) return st;
-    ctx->launches += 2;
     MIRROR_CUDA_OK(cudaGetLastError());
     return MIRROR_OK;
 }
