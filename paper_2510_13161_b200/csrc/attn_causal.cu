@@ -6,7 +6,8 @@
 // units form one sequence that is split evenly over the CTAs.  Within a CTA each of four warps is on its own: it takes every fourth slot of the
 // CTA's range, keeps two slots on the way with TMA (a ring of its own: no barrier but its own), multiplies them with mma.sync (16 rows are
 // what it has; a tcgen05 tile would be 128) and holds its running maximum, sum and accumulator in registers.  At the end of a unit the
-// four are merged in shared memory; two CTAs share an SM, so that one's merge hides behind the other's stream.  A unit that the partition cut
+// four are added up in shared memory, one after the other; three or four CTAs share an SM, so that one's chains of dependent steps (and its
+// merges) hide behind the others' streams.  A unit that the partition cut
 // leaves a record per part for attn_token_merge_kernel.
 // P is multiplied as the sum of two bf16 (its rounding and what that left): the tensor cores have the time, and the output then carries no
 // rounding but its own.
@@ -20,24 +21,28 @@ namespace {
 
 using causal::Request;
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 2;                          // slots a warp has on the way
 constexpr int kRows = 16;
+constexpr int kMaxCtas = 768;                       // (notes of 16 bytes each, in 12 KB)
 constexpr int kMergeThreads = 256;
+constexpr size_t kSmemPerSm = 233472;               // 228 KB, of which every CTA takes 1 KB more than it asks for
 constexpr float kLazy = 8.f;                        // the running maximum moves when a score passes it by this (log2): P stays below 2^8
+constexpr int kUnitSlots = 10;                       // what a unit costs beside its slots (queries, the merge of the warps, the output)
 constexpr int kMinShare = 16;                       // slots of a CTA at least, where units are cut
 
-template <int D>
+template <int D, int kWarps>
 struct Cfg {
+    static constexpr int kThreads = 32 * kWarps;
+    static constexpr int kAreas = kWarps / 4;                       // where four warps each add up what they have
     static constexpr int kHalves = D / 64;
     static constexpr int kSlotBytes = kAttnSlotTok * D * 2;
     static constexpr int kRec = kRows * D + 2 * kRows;              // record: accumulators, maxima, sums
     static constexpr int kPitch = D + 4;                            // floats of a row in the merge area
     static constexpr int kRing = kWarps * kStages * 2 * kSlotBytes;
-    static constexpr int kMerge = kWarps * kRows * (kPitch + 2) * 4;
+    static constexpr int kMerge = kAreas * kRows * kPitch * 4 + kWarps * kRows * 2 * 4;
+    static constexpr int kCtas = kWarps > 4 ? 1 : D == 128 ? 3 : 4; // of an SM, by registers
     static constexpr int kBars = kWarps * kStages * 8;
-    static size_t smem(int B) { return (size_t)kRing + kMerge + kBars + 64 + (4 * (size_t)B + 1) * 4; }
+    static size_t smem(int B) { return (size_t)kRing + kMerge + kBars + 64 + (5 * (size_t)B + 2) * 4; }
 };
 
 struct TokenMaps {
@@ -45,41 +50,46 @@ struct TokenMaps {
 };
 
 struct Begin {
-    long long x;
+    long long x;                          // slots ahead of it
     int layer, b, h, t;
 };
-// Where CTA c's range begins.  never_cut: at a unit's first slot; else even shares, moved to a unit boundary close by (a cut costs a record
-// and a merge).
-__device__ Begin range_begin(const CausalParams& p, const int* cum, long long total, int ctas, int c, bool never_cut) {
-    Begin u = {c <= 0 ? 0 : total, 0, 0, 0, 0};
+// Slots of a head's units, and how many units have any, summed over the requests.
+struct Sums {
+    const int *slots, *units;             // [B + 1] each
+    __device__ __forceinline__ int cost(int b) const { return slots[b] + kUnitSlots * units[b]; }
+};
+// Where CTA c's range begins.  The sequence is split evenly by cost, kUnitSlots for a unit and one for each of its slots.  never_cut: a range
+// begins with a unit; else a boundary close to a unit's is moved there (a cut costs a record and a merge).
+__device__ Begin range_begin(const CausalParams& p, const Sums& s, long long total, int ctas, int c, bool never_cut) {
+    const long long per_layer = (long long)p.Hkv * s.slots[p.B];
+    Begin u = {c <= 0 ? 0 : per_layer * p.L, 0, 0, 0, 0};
     if (c <= 0 || c >= ctas) return u;
-    const long long per_layer = (long long)p.Hkv * cum[p.B], share = total / ctas;
-    u.x = total * c / ctas;
-    u.layer = (int)(u.x / per_layer);
-    const long long rem = u.x - u.layer * per_layer;
-    int lo = 0, hi = p.B - 1;                                      // the first b with Hkv * cum[b + 1] > rem
+    const long long cost_layer = (long long)p.Hkv * s.cost(p.B), x = total * c / ctas;
+    u.layer = (int)(x / cost_layer);
+    const long long rem = x - u.layer * cost_layer;
+    int lo = 0, hi = p.B - 1;                                      // the first b with Hkv * cost(b + 1) > rem
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if ((long long)p.Hkv * cum[mid + 1] > rem) hi = mid; else lo = mid + 1;
+        if ((long long)p.Hkv * s.cost(mid + 1) > rem) hi = mid; else lo = mid + 1;
     }
     u.b = lo;
-    const int T = cum[lo + 1] - cum[lo];
-    const int in = (int)(rem - (long long)p.Hkv * cum[lo]);
-    u.h = in / T;
-    u.t = in - u.h * T;
-    const int tol = (int)min(8ll, share >> 2);
-    if (u.t == 0) return u;
-    if (!never_cut && u.t <= tol) {
-        u.x -= u.t;
-        u.t = 0;
-    } else if (never_cut || T - u.t <= tol) {
-        u.x += T - u.t;
+    const int T = s.slots[lo + 1] - s.slots[lo], per = T + kUnitSlots;
+    const int in = (int)(rem - (long long)p.Hkv * s.cost(lo));
+    u.h = in / per;
+    u.t = max(0, in - u.h * per - kUnitSlots);
+    const int tol = (int)min(8ll, total / ctas >> 2);
+    if (!never_cut && u.t <= tol) u.t = 0;
+    // (never cut: the unit belongs to the CTA that has its larger part)
+    if (u.t > 0 && (never_cut ? 2 * (in - u.h * per) > per : T - u.t <= tol)) u.t = T;
+    if (never_cut && u.t < T) u.t = 0;
+    u.x = u.layer * per_layer + (long long)p.Hkv * s.slots[lo] + (long long)u.h * T + u.t;
+    if (u.t == T) {
         u.t = 0;
         if (++u.h == p.Hkv) {
             u.h = 0;
             do {
                 if (++u.b == p.B) { u.b = 0; ++u.layer; }
-            } while (u.layer < p.L && cum[u.b + 1] == cum[u.b]);
+            } while (u.layer < p.L && s.slots[u.b + 1] == s.slots[u.b]);
         }
     }
     return u;
@@ -104,16 +114,18 @@ struct Cursor {
     Request r;
 };
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_constant__ TokenMaps tm, const __grid_constant__ CausalParams p, const int never_cut) {
-    using C = Cfg<D>;
+template <int D, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, Cfg<D, kWarps>::kCtas) attn_token_kernel(const __grid_constant__ TokenMaps tm, const __grid_constant__ CausalParams p, const int never_cut) {
+    using C = Cfg<D, kWarps>;
+    constexpr int kThreads = C::kThreads;
     extern __shared__ __align__(1024) uint8_t smem[];
-    float* const s_o = (float*)(smem + C::kRing);                   // [warps][16][pitch], then [warps][16][max, sum]
-    float* const s_ml = s_o + kWarps * kRows * C::kPitch;
+    float* const s_o = (float*)(smem + C::kRing);                   // [areas][16][pitch], then [warps][16][max, sum]
+    float* const s_ml = s_o + C::kAreas * kRows * C::kPitch;
     uint64_t* const bars = (uint64_t*)(smem + C::kRing + C::kMerge);
     Begin* const s_begin = (Begin*)(bars + kWarps * kStages);       // 2 x 24 bytes
     int* const cum = (int*)((uint8_t*)bars + C::kBars + 64);        // [B + 1] slots of a head's units, summed over the requests
-    int* const s_row0 = cum + p.B + 1;                              // [B] each
+    int* const cum_units = cum + p.B + 1;                           // [B + 1] units that have any
+    int* const s_row0 = cum_units + p.B + 1;                        // [B] each
     int* const s_n = s_row0 + p.B;
     int* const s_prefix = s_n + p.B;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -124,10 +136,9 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
         if (warp == 0) { ptx::prefetch_tmap(&tm.k); ptx::prefetch_tmap(&tm.v); }
     }
     ptx::grid_dep_wait();
-    ptx::grid_dep_launch();
     if (warp == 0) {
         int acc = 0, units = 0;
-        if (lane == 0) cum[0] = 0;
+        if (lane == 0) cum[0] = cum_units[0] = 0;
         for (int b0 = 0; b0 < p.B; b0 += 32) {
             const int b = b0 + lane;
             int row0 = 0, n = 0, prefix = 0, sum = 0;
@@ -136,7 +147,9 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
                 sum = max(causal::make_request(p, row0, n, prefix).slots, 0);
                 s_row0[b] = row0; s_n[b] = n; s_prefix[b] = prefix;
             }
-            units += __popc(__ballot_sync(0xffffffffu, sum > 0));
+            const uint32_t some = __ballot_sync(0xffffffffu, sum > 0);
+            if (b < p.B) cum_units[b + 1] = units + __popc(some & (0xffffffffu >> (31 - lane)));
+            units += __popc(some);
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int v = __shfl_up_sync(0xffffffffu, sum, o);
@@ -146,14 +159,14 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
             acc += __shfl_sync(0xffffffffu, sum, 31);
         }
         __syncwarp();
-        const long long total = (long long)p.L * p.Hkv * acc;
-        const long long most = max((long long)units * p.L * p.Hkv, total / kMinShare);
+        const Sums sums = {cum, cum_units};
+        const long long lh = (long long)p.L * p.Hkv, total = lh * (acc + kUnitSlots * units), most = max(lh * units, lh * acc / kMinShare);
         const int ctas = (int)min((long long)gridDim.x, max(most, 1ll));
         if (lane < 2) {
-            s_begin[lane] = range_begin(p, cum, total, ctas, (int)blockIdx.x + lane, never_cut != 0);
+            s_begin[lane] = range_begin(p, sums, total, ctas, (int)blockIdx.x + lane, never_cut != 0);
             if (lane == 0 && !never_cut) {
                 const Begin& u = s_begin[0];
-                p.begins[blockIdx.x] = {u.x < total && u.t > 0 ? 1 : 0, u.layer, u.b, u.h};
+                p.begins[blockIdx.x] = {u.t > 0 ? 1 : 0, u.layer, u.b, u.h};
             }
         }
     }
@@ -234,23 +247,25 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
     const int v_tok = lane & 15, v_chunk = lane >> 4;
     Cursor cc;
     start(cc);
-    for (;;) {
-        // a unit's part: queries
-        uint32_t qf[D / 16][4];
-        const int rows = cc.r.n * p.G;
-        const int i0 = g / p.G, i1 = (g + 8) / p.G;
-        {
-            const __nv_bfloat16* const qb = p.q + (((size_t)cc.layer * p.R + cc.r.row0) * p.Hq + cc.h * p.G) * D;
-            const __nv_bfloat16* const q0 = qb + ((size_t)i0 * p.Hq + (g - i0 * p.G)) * D;
-            const __nv_bfloat16* const q1 = qb + ((size_t)i1 * p.Hq + (g + 8 - i1 * p.G)) * D;
+    uint32_t qf[D / 16][4];
+    const int i0 = g / p.G, i1 = (g + 8) / p.G;
+    auto load_q = [&](const Cursor& c) {                            // a unit's queries
+        const int rows = c.r.n * p.G;
+        const __nv_bfloat16* const qb = p.q + (((size_t)c.layer * p.R + c.r.row0) * p.Hq + c.h * p.G) * D + c2;
+        const __nv_bfloat16* const q0 = qb + ((size_t)i0 * p.Hq + (g - i0 * p.G)) * D;
+        const __nv_bfloat16* const q1 = qb + ((size_t)i1 * p.Hq + (g + 8 - i1 * p.G)) * D;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                qf[k][0] = g < rows ? *reinterpret_cast<const uint32_t*>(q0 + k * 16 + c2) : 0u;
-                qf[k][1] = g + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + k * 16 + c2) : 0u;
-                qf[k][2] = g < rows ? *reinterpret_cast<const uint32_t*>(q0 + k * 16 + 8 + c2) : 0u;
-                qf[k][3] = g + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + k * 16 + 8 + c2) : 0u;
-            }
+        for (int k = 0; k < D / 16; ++k) {
+            qf[k][0] = g < rows ? *reinterpret_cast<const uint32_t*>(q0 + k * 16) : 0u;
+            qf[k][1] = g + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + k * 16) : 0u;
+            qf[k][2] = g < rows ? *reinterpret_cast<const uint32_t*>(q0 + k * 16 + 8) : 0u;
+            qf[k][3] = g + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + k * 16 + 8) : 0u;
         }
+    };
+    load_q(cc);
+    for (;;) {
+        // a unit's part
+        const int rows = cc.r.n * p.G;
         float o[D / 8][4];
 #pragma unroll
         for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
@@ -280,14 +295,25 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
                 ptx::fence_proxy_async();                           // (the stage's next copy comes behind these)
                 __syncwarp();
             }
-            float sc[2][4] = {};
+            // (all of a slot's loads are issued ahead of the products that wait for them)
+            float sc[2][4] = {}, sd[2][4] = {};
+            uint32_t kf[D / 16][4];
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                uint32_t b[4];
-                ldmatrix4(b, ka + attn::kv_slot_off<C::kHalves>(k_tok, 2 * k + k_chunk));
-                mma16816(sc[0], qf[k], b[0], b[1]);
-                mma16816(sc[1], qf[k], b[2], b[3]);
+            for (int k = 0; k < D / 16; ++k) ldmatrix4(kf[k], ka + attn::kv_slot_off<C::kHalves>(k_tok, 2 * k + k_chunk));
+#pragma unroll
+            for (int k = 0; k < D / 16; k += 2) {
+                mma16816(sc[0], qf[k], kf[k][0], kf[k][1]);
+                mma16816(sc[1], qf[k], kf[k][2], kf[k][3]);
+                mma16816(sd[0], qf[k + 1], kf[k + 1][0], kf[k + 1][1]);
+                mma16816(sd[1], qf[k + 1], kf[k + 1][2], kf[k + 1][3]);
             }
+            uint32_t vf[D / 32][4];
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) ldmatrix4t(vf[j], va + attn::kv_slot_off<C::kHalves>(v_tok, 2 * j + v_chunk));
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[j][e] += sd[j][e];
             const bool all_seen = key0 + kAttnSlotTok - 1 <= cc.r.prefix &&
                                   (p.window == 0 || key0 > pos_last - p.window || key0 + kAttnSlotTok <= p.n_sink);
             if (!all_seen) {
@@ -301,14 +327,12 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
                         if (key > pos1 || !(sink || key > pos1 - p.window)) sc[j][2 + e] = -INFINITY;
                     }
             }
-            float x0 = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]));
-            float x1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]));
-            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1)); x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
-            x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2)); x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-            x0 *= p.scale_log2e;
-            x1 *= p.scale_log2e;
-            const bool up0 = x0 > m0 + kLazy, up1 = x1 > m1 + kLazy;
-            if (__any_sync(0xffffffffu, up0 || up1)) {
+            float x0 = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1])) * p.scale_log2e;
+            float x1 = fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3])) * p.scale_log2e;
+            if (__any_sync(0xffffffffu, x0 > m0 + kLazy || x1 > m1 + kLazy)) {
+                x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1)); x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+                x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2)); x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+                const bool up0 = x0 > m0 + kLazy, up1 = x1 > m1 + kLazy;
                 const float a0 = up0 ? exp2f(m0 - x0) : 1.f, a1 = up1 ? exp2f(m1 - x1) : 1.f;
                 if (up0) m0 = x0;
                 if (up1) m1 = x1;
@@ -331,55 +355,86 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
                 pl[2 * j + 1] = attn::pack_bf16(e2 - __uint_as_float(ph[2 * j + 1] << 16), e3 - __uint_as_float(ph[2 * j + 1] & 0xffff0000u));
             }
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
-                uint32_t b[4];
-                ldmatrix4t(b, va + attn::kv_slot_off<C::kHalves>(v_tok, 2 * j + v_chunk));
-                mma16816(o[2 * j], ph, b[0], b[1]);
-                mma16816(o[2 * j + 1], ph, b[2], b[3]);
-                mma16816(o[2 * j], pl, b[0], b[1]);
-                mma16816(o[2 * j + 1], pl, b[2], b[3]);
+            for (int j0 = 0; j0 < D / 16; j0 += D / 32) {
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) {
+                    mma16816(o[2 * (j0 + j)], ph, vf[j][0], vf[j][1]);
+                    mma16816(o[2 * (j0 + j) + 1], ph, vf[j][2], vf[j][3]);
+                }
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) {
+                    mma16816(o[2 * (j0 + j)], pl, vf[j][0], vf[j][1]);
+                    mma16816(o[2 * (j0 + j) + 1], pl, vf[j][2], vf[j][3]);
+                }
+                if (j0 == 0) {
+#pragma unroll
+                    for (int j = 0; j < D / 32; ++j) ldmatrix4t(vf[j], va + attn::kv_slot_off<C::kHalves>(v_tok, 2 * (D / 32 + j) + v_chunk));
+                }
             }
             __syncwarp();
             issue();
         }
-        // ---- the part's end: the warps' accumulators are merged
+        // ---- the part's end: the warps' accumulators are merged (the next unit's queries are on the way meanwhile)
+        const Cursor was = cc;
+        const bool last = cc.left <= 0;
+        if (!last) {
+            next_unit(cc);
+            load_q(cc);
+        }
         l0 += __shfl_xor_sync(0xffffffffu, l0, 1); l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
         l0 += __shfl_xor_sync(0xffffffffu, l0, 2); l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
-        {
-            float* const w_o = s_o + warp * kRows * C::kPitch;
-#pragma unroll
-            for (int j = 0; j < D / 8; ++j) {
-                if (g < rows) *reinterpret_cast<float2*>(w_o + g * C::kPitch + j * 8 + c2) = make_float2(o[j][0], o[j][1]);
-                if (g + 8 < rows) *reinterpret_cast<float2*>(w_o + (g + 8) * C::kPitch + j * 8 + c2) = make_float2(o[j][2], o[j][3]);
-            }
-            if (c2 == 0) {
-                float* const ml = s_ml + warp * kRows * 2;
-                ml[g * 2] = m0; ml[g * 2 + 1] = l0;
-                ml[(g + 8) * 2] = m1; ml[(g + 8) * 2 + 1] = l1;
-            }
+        if (c2 == 0) {
+            float* const ml = s_ml + warp * kRows * 2;
+            ml[g * 2] = m0; ml[g * 2 + 1] = l0;
+            ml[(g + 8) * 2] = m1; ml[(g + 8) * 2 + 1] = l1;
         }
         __syncthreads();
-        const bool whole = t_first == 0 && cc.t_end == cc.r.slots;
+        // the warps bring their accumulators to the common maximum and add them up, one after the other
+        float M0 = -INFINITY, M1 = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            M0 = fmaxf(M0, s_ml[(w * kRows + g) * 2]);
+            M1 = fmaxf(M1, s_ml[(w * kRows + g + 8) * 2]);
+        }
+        const float f0 = m0 == -INFINITY ? 0.f : exp2f(m0 - M0), f1 = m1 == -INFINITY ? 0.f : exp2f(m1 - M1);
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+            if (w == (warp & 3)) {
+                float* const area = s_o + (warp >> 2) * kRows * C::kPitch;
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) {
+                    float2* const a = reinterpret_cast<float2*>(area + g * C::kPitch + j * 8 + c2);
+                    float2* const b = reinterpret_cast<float2*>(area + (g + 8) * C::kPitch + j * 8 + c2);
+                    const float2 x = w ? *a : make_float2(0.f, 0.f);
+                    if (g < rows) *a = make_float2(fmaf(f0, o[j][0], x.x), fmaf(f0, o[j][1], x.y));
+                    const float2 y = w ? *b : make_float2(0.f, 0.f);
+                    if (g + 8 < rows) *b = make_float2(fmaf(f1, o[j][2], y.x), fmaf(f1, o[j][3], y.y));
+                }
+            }
+            __syncthreads();
+        }
+        const bool whole = t_first == 0 && was.t_end == was.r.slots;
         float* const rec = p.partial + ((size_t)blockIdx.x * 2 + (t_first > 0 ? 0 : 1)) * C::kRec;
         for (int i = tid; i < rows * (D / 4); i += kThreads) {
             const int row = i / (D / 4), col = (i % (D / 4)) * 4;
             float M = -INFINITY, Ls = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_ml[(w * kRows + row) * 2]);
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float mw = s_ml[(w * kRows + row) * 2];
-                if (mw == -INFINITY) continue;
-                const float f = exp2f(mw - M);
-                const float4 v = *reinterpret_cast<const float4*>(s_o + (w * kRows + row) * C::kPitch + col);
-                Ls = fmaf(f, s_ml[(w * kRows + row) * 2 + 1], Ls);
-                acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+                if (mw != -INFINITY) Ls = fmaf(exp2f(mw - M), s_ml[(w * kRows + row) * 2 + 1], Ls);
+            }
+            float4 acc = *reinterpret_cast<const float4*>(s_o + row * C::kPitch + col);
+#pragma unroll
+            for (int a = 1; a < C::kAreas; ++a) {
+                const float4 v = *reinterpret_cast<const float4*>(s_o + (a * kRows + row) * C::kPitch + col);
+                acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
             }
             if (whole) {
                 const float inv = 1.f / Ls;
-                const int it = row / p.G, head = cc.h * p.G + row - it * p.G;
-                const size_t at = ((size_t)cc.layer * p.R + cc.r.row0 + it) * p.Hq + head;
+                const int it = row / p.G, head = was.h * p.G + row - it * p.G;
+                const size_t at = ((size_t)was.layer * p.R + was.r.row0 + it) * p.Hq + head;
                 *reinterpret_cast<uint2*>(p.out + at * D + col) = make_uint2(attn::pack_bf16(acc.x * inv, acc.y * inv), attn::pack_bf16(acc.z * inv, acc.w * inv));
                 if (p.lse_out && col == 0) p.lse_out[at] = M * kAttnLn2 + logf(Ls);
             } else {
@@ -387,9 +442,8 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
                 if (col == 0) { rec[kRows * D + row] = M; rec[kRows * D + kRows + row] = Ls; }
             }
         }
-        if (cc.left <= 0) break;
+        if (last) break;
         __syncthreads();                                            // (the merge area is written again)
-        next_unit(cc);
     }
     if (dead) {
         // copies on the way land before the CTA's shared memory goes away
@@ -398,14 +452,14 @@ __global__ void __launch_bounds__(kThreads) attn_token_kernel(const __grid_const
 }
 
 // The units that the partition cut.  A block per boundary; the blocks whose boundaries cut one unit share its merge by runs of four
-// columns, a warp to each, a lane to a part.
+// columns, a thread to each.  What takes the time is one trip to L2 after another, so a thread asks for kMergeBatch parts at once.
+constexpr int kMergeBatch = 4;
 template <int D>
 __global__ void __launch_bounds__(kMergeThreads) attn_token_merge_kernel(const __grid_constant__ CausalParams p, const int ctas) {
-    using C = Cfg<D>;
-    __shared__ attn::GroupBegin s_begin[1024];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, at = blockIdx.x + 1;
+    constexpr int kRec = kRows * D + 2 * kRows;
+    __shared__ attn::GroupBegin s_begin[kMaxCtas];
+    const int tid = threadIdx.x, at = blockIdx.x + 1;
     ptx::grid_dep_wait();
-    ptx::grid_dep_launch();
     for (int i = tid; i < ctas; i += kMergeThreads) s_begin[i] = p.begins[i];
     __syncthreads();
     const attn::GroupBegin u = s_begin[at];
@@ -417,54 +471,80 @@ __global__ void __launch_bounds__(kMergeThreads) attn_token_merge_kernel(const _
     const int parts = gb - ga + 1, blocks = parts - 1, mine = at - (ga + 1);
     int row0, n, prefix;
     causal::load_request(p, u.b, row0, n, prefix, false);
-    for (int i = mine * (kMergeThreads / 32) + warp; i < n * p.G * (D / 4); i += blocks * (kMergeThreads / 32)) {
+    // lanes to a run of columns: as many as there are threads for, each with every S-th part
+    const int items = n * p.G * (D / 4);
+    int S = 1;
+    while (S < 32 && 2 * S <= parts && 2 * S * items <= blocks * kMergeThreads) S <<= 1;
+    const int lane_s = tid & (S - 1), per_block = kMergeThreads / S;
+    for (int i0 = mine * per_block; i0 < items; i0 += blocks * per_block) {
+        const int i = min(i0 + tid / S, items - 1);                 // (groups behind the last one do its work, too)
         const int row = i / (D / 4), col = (i % (D / 4)) * 4;
-        float M = -INFINITY;
-        for (int k = lane; k < parts; k += 32) M = fmaxf(M, p.partial[((size_t)(ga + k) * 2 + (k == 0)) * C::kRec + kRows * D + row]);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        float L = 0.f;
+        float M = -INFINITY, L = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = lane; k < parts; k += 32) {
-            const float* rec = p.partial + ((size_t)(ga + k) * 2 + (k == 0)) * C::kRec;
-            const float m = rec[kRows * D + row];
-            if (m == -INFINITY) continue;
-            const float f = exp2f(m - M);
-            const float4 v = *reinterpret_cast<const float4*>(rec + row * D + col);
-            L = fmaf(f, rec[kRows * D + kRows + row], L);
-            acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
-        }
+        for (int k0 = lane_s; k0 < parts; k0 += kMergeBatch * S) {
+            float m[kMergeBatch], l[kMergeBatch];
+            float4 v[kMergeBatch];
 #pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            L += __shfl_xor_sync(0xffffffffu, L, d);
-            acc.x += __shfl_xor_sync(0xffffffffu, acc.x, d); acc.y += __shfl_xor_sync(0xffffffffu, acc.y, d);
-            acc.z += __shfl_xor_sync(0xffffffffu, acc.z, d); acc.w += __shfl_xor_sync(0xffffffffu, acc.w, d);
+            for (int k = 0; k < kMergeBatch; ++k) {                 // (all loads of a batch are on the way at once)
+                const int part = k0 + k * S;
+                const float* rec = p.partial + ((size_t)(ga + part) * 2 + (part == 0)) * kRec;
+                const bool in = part < parts;
+                m[k] = in ? rec[kRows * D + row] : -INFINITY;
+                l[k] = in ? rec[kRows * D + kRows + row] : 0.f;
+                v[k] = in ? *reinterpret_cast<const float4*>(rec + row * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            float top = M;
+#pragma unroll
+            for (int k = 0; k < kMergeBatch; ++k) top = fmaxf(top, m[k]);
+            if (top == -INFINITY) continue;
+            const float keep = exp2f(M - top);
+            M = top;
+            L *= keep;
+            acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
+#pragma unroll
+            for (int k = 0; k < kMergeBatch; ++k) {
+                const float f = exp2f(m[k] - top);                  // (a part that saw nothing: 0)
+                L = fmaf(f, l[k], L);
+                acc.x = fmaf(f, v[k].x, acc.x); acc.y = fmaf(f, v[k].y, acc.y); acc.z = fmaf(f, v[k].z, acc.z); acc.w = fmaf(f, v[k].w, acc.w);
+            }
         }
-        if (lane == 0) {
-            const float inv = 1.f / L;
-            const int it = row / p.G, head = u.g * p.G + row - it * p.G;
-            const size_t o = ((size_t)u.layer * p.R + row0 + it) * p.Hq + head;
-            *reinterpret_cast<uint2*>(p.out + o * D + col) = make_uint2(attn::pack_bf16(acc.x * inv, acc.y * inv), attn::pack_bf16(acc.z * inv, acc.w * inv));
-            if (p.lse_out && col == 0) p.lse_out[o] = M * kAttnLn2 + logf(L);
+        if (S > 1) {
+            float top = M;
+            for (int d = 1; d < S; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float f = M == -INFINITY ? 0.f : exp2f(M - top);
+            M = top;
+            L *= f;
+            acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+            for (int d = 1; d < S; d <<= 1) {
+                L += __shfl_xor_sync(0xffffffffu, L, d);
+                acc.x += __shfl_xor_sync(0xffffffffu, acc.x, d); acc.y += __shfl_xor_sync(0xffffffffu, acc.y, d);
+                acc.z += __shfl_xor_sync(0xffffffffu, acc.z, d); acc.w += __shfl_xor_sync(0xffffffffu, acc.w, d);
+            }
         }
+        if (lane_s != 0 || i0 + tid / S >= items) continue;
+        const float inv = 1.f / L;
+        const int it = row / p.G, head = u.g * p.G + row - it * p.G;
+        const size_t o = ((size_t)u.layer * p.R + row0 + it) * p.Hq + head;
+        *reinterpret_cast<uint2*>(p.out + o * D + col) = make_uint2(attn::pack_bf16(acc.x * inv, acc.y * inv), attn::pack_bf16(acc.z * inv, acc.w * inv));
+        if (p.lse_out && col == 0) p.lse_out[o] = M * kAttnLn2 + logf(L);
     }
 }
 
-template <int D>
-mirror_status token_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& p, cudaStream_t stream) {
-    using C = Cfg<D>;
+template <int D, int kWarps>
+mirror_status token_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& p, size_t records_bytes, cudaStream_t stream) {
+    using C = Cfg<D, kWarps>;
     TokenMaps tm;
     mirror_status st = mirror_attn_pool_tmap(ctx, kv, kv->k_pool, &tm.k);
     if (st == MIRROR_OK) st = mirror_attn_pool_tmap(ctx, kv, kv->v_pool, &tm.v);
     if (st != MIRROR_OK) return st;
     // Units of at most 32 slots take a CTA less time whole (8 slots a warp) than a launch that merges their parts.
     const int never_cut = causal_most_slots(p, p.max_rows) <= 32;
-    const int ctas = 2 * ctx->num_sms;
-    static_assert(sizeof(attn::GroupBegin) == 16, "notes");
-    if (ctas > 1024 || (size_t)ctas * sizeof(attn::GroupBegin) > kWsNotesBytes) return MIRROR_ERR_SHAPE;
     const size_t smem = C::smem(p.B);
-    MIRROR_CUDA_OK(cudaFuncSetAttribute(attn_token_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    MIRROR_CUDA_OK(mirror_launch_pdl(attn_token_kernel<D>, dim3((unsigned)ctas), dim3(kThreads), smem, stream, tm, p, never_cut));
+    const int ctas = ctx->num_sms * std::max(1, std::min((int)C::kCtas, (int)(kSmemPerSm / (smem + 1024))));
+    static_assert(sizeof(attn::GroupBegin) == 16, "notes");
+    if (ctas > kMaxCtas || (size_t)ctas * 2 * C::kRec * sizeof(float) > records_bytes) return MIRROR_ERR_SHAPE;
+    MIRROR_CUDA_OK(cudaFuncSetAttribute(attn_token_kernel<D, kWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    MIRROR_CUDA_OK(mirror_launch_pdl(attn_token_kernel<D, kWarps>, dim3((unsigned)ctas), dim3(C::kThreads), smem, stream, tm, p, never_cut));
     ctx->launches += 1;
     if (!never_cut) {
         MIRROR_CUDA_OK(mirror_launch_pdl(attn_token_merge_kernel<D>, dim3((unsigned)(ctas - 1)), dim3(kMergeThreads), 0, stream, p, ctas));
@@ -487,9 +567,6 @@ mirror_status mirror_attn_pool_tmap(const mirror_ctx* ctx, const mirror_kv* kv, 
     return mirror_make_tmap(ctx, map, pool, 5, dims, strides, box);
 }
 
-mirror_status mirror_attn_token_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& p, cudaStream_t stream) {
-    return ctx->desc.head_dim == 128 ? token_launch<128>(ctx, kv, p, stream) : token_launch<64>(ctx, kv, p, stream);
-}
 
 extern "C" mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, const mirror_rows* rows, size_t* bytes) {
     if (!ctx || !bytes) return MIRROR_ERR_ARG;
@@ -497,7 +574,7 @@ extern "C" mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, cons
     if (st != MIRROR_OK) return st;
     MirrorWsLayout L;
     mirror_ws_layout(ctx, 1, &L);
-    *bytes = align_up(L.end_attn, 256) + mirror_attn_prompt_plan_bytes(ctx, rows);
+    *bytes = align_up(L.end_attn, 256) + std::max(mirror_attn_prompt_plan_bytes(ctx), kMaxCtas * sizeof(attn::GroupBegin));
     return MIRROR_OK;
 }
 
@@ -535,6 +612,13 @@ extern "C" mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv
     p.partial = (float*)(ws + L.attn_partial);
     p.status = ctx->d_status;
     p.wait_limit = ctx->tune.wait_limit_cycles;
-    if ((int64_t)p.max_rows * p.G <= kRows) return mirror_attn_token_launch(ctx, kv, p, (cudaStream_t)stream);
-    return mirror_attn_prompt_launch(ctx, kv, p, ws + align_up(L.end_attn, 256), (cudaStream_t)stream);
+    void* const notes = ws + align_up(L.end_attn, 256);
+    if ((int64_t)p.max_rows * p.G <= kRows) {
+        p.begins = (attn::GroupBegin*)notes;
+        // Fewer units than SMs: one CTA of twelve warps to an SM, else three or four of four.  (Measured below.)
+        const bool few = (int64_t)p.L * p.B * p.Hkv <= ctx->num_sms;
+        auto launch = ctx->desc.head_dim == 128 ? (few ? token_launch<128, 12> : token_launch<128, 4>) : (few ? token_launch<64, 12> : token_launch<64, 4>);
+        return launch(ctx, kv, p, L.attn_partial_bytes, (cudaStream_t)stream);
+    }
+    return mirror_attn_prompt_launch(ctx, kv, p, notes, (cudaStream_t)stream);
 }

@@ -29,9 +29,8 @@ static inline long long causal_most_slots(const CausalParams& p, int rows) {    
     }
     return s;
 }
-mirror_status mirror_attn_token_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& p, cudaStream_t stream);
 mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalParams& p, void* plan, cudaStream_t stream);
-size_t mirror_attn_prompt_plan_bytes(const mirror_ctx* ctx, const mirror_rows* rows);
+size_t mirror_attn_prompt_plan_bytes(const mirror_ctx* ctx);
 // pool as (64 columns, 8 tokens, D/64 halves, 2 token groups, (layer*page)*head): one box is one page of one head, landing as
 // [token / 8][half][token % 8][128 B]
 mirror_status mirror_attn_pool_tmap(const mirror_ctx* ctx, const mirror_kv* kv, const void* pool, CUtensorMap* map);

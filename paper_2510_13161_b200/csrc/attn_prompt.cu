@@ -894,8 +894,7 @@ void row_tile(int G, int* gs, int* shares, int* nt) {
 }
 }  // namespace
 
-size_t mirror_attn_prompt_plan_bytes(const mirror_ctx* ctx, const mirror_rows* rows) {
-    (void)rows;
+size_t mirror_attn_prompt_plan_bytes(const mirror_ctx* ctx) {
     return align_up((size_t)ctx->num_sms * sizeof(Unit), 256);
 }
 
