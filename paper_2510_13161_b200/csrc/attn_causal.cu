@@ -3,12 +3,16 @@
 // attn_token_kernel: requests with at most 16 rows per KV head (rows x query heads of the group), single tokens above all.  Each byte of the
 // cache is used for 16 rows at most, so HBM bounds it, and what counts is that every SM always has enough bytes on the way (45 KB,
 // Little's law at 6.5 TB/s and ~1 us).  The 16-token slots (one page of one head: 4 KB of K and of V at d = 128) of all (layer, request, head)
-// units form one sequence that is split evenly over the CTAs.  Within a CTA each of four warps is on its own: it takes every fourth slot of the
-// CTA's range, keeps two slots on the way with TMA (a ring of its own: no barrier but its own), multiplies them with mma.sync (16 rows are
-// what it has; a tcgen05 tile would be 128) and holds its running maximum, sum and accumulator in registers.  At the end of a unit the
-// four are added up in shared memory, one after the other; three or four CTAs share an SM, so that one's chains of dependent steps (and its
-// merges) hide behind the others' streams.  A unit that the partition cut
-// leaves a record per part for attn_token_merge_kernel.
+// units form one sequence that is split evenly over the CTAs by what units cost.  Within a CTA every warp streams for itself: of each unit it
+// takes every fourth slot (or twelfth), keeps two on the way with TMA (a ring of its own: no barrier but its own), multiplies them with
+// mma.sync (16 rows are what it has; a tcgen05 tile would be 128) and holds its running maximum, sum and accumulator in registers.  At the
+// end of a unit the warps' accumulators are added up in shared memory, one after the other; three or four CTAs share an SM, so that one's
+// chains of dependent steps, and its merges, hide behind the others' streams.  A unit that the partition cut leaves a record per part for
+// attn_token_merge_kernel.  Tried and no faster: two slots at a time (the same instructions, less overlap), and ranges of whole warps
+// without barriers between units (more parts).
+//
+// Neither kernel lets the one behind it start early: CTAs of the next call that find room beside the last ones of this call leave the SMs
+// with unequal numbers of equal shares (48 requests under a window, call after call: 178 us, else 130).
 // P is multiplied as the sum of two bf16 (its rounding and what that left): the tensor cores have the time, and the output then carries no
 // rounding but its own.
 #include <math.h>
@@ -27,7 +31,7 @@ constexpr int kMaxCtas = 768;                       // (notes of 16 bytes each, 
 constexpr int kMergeThreads = 256;
 constexpr size_t kSmemPerSm = 233472;               // 228 KB, of which every CTA takes 1 KB more than it asks for
 constexpr float kLazy = 8.f;                        // the running maximum moves when a score passes it by this (log2): P stays below 2^8
-constexpr int kUnitSlots = 10;                       // what a unit costs beside its slots (queries, the merge of the warps, the output)
+constexpr int kUnitSlots = 10;                      // what a unit costs beside its slots (queries, the merge of the warps, the output)
 constexpr int kMinShare = 16;                       // slots of a CTA at least, where units are cut
 
 template <int D, int kWarps>
@@ -615,8 +619,10 @@ extern "C" mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv
     void* const notes = ws + align_up(L.end_attn, 256);
     if ((int64_t)p.max_rows * p.G <= kRows) {
         p.begins = (attn::GroupBegin*)notes;
-        // Fewer units than SMs: one CTA of twelve warps to an SM, else three or four of four.  (Measured below.)
-        const bool few = (int64_t)p.L * p.B * p.Hkv <= ctx->num_sms;
+        // Units that are few, a quarter of the SMs at most, get one CTA of twelve warps per SM: a third of the parts to merge, and a short unit
+        // is over sooner (32768 tokens x 8 heads 39.6 -> 35.0 us, 300 tokens 11.2 -> 10.1).  Else three or four CTAs of four warps, of which
+        // some stream while others merge (96 units of up to 66 slots: 20.4 against 28.2 us).
+        const bool few = (int64_t)p.L * p.B * p.Hkv * 4 <= ctx->num_sms;
         auto launch = ctx->desc.head_dim == 128 ? (few ? token_launch<128, 12> : token_launch<128, 4>) : (few ? token_launch<64, 12> : token_launch<64, 4>);
         return launch(ctx, kv, p, L.attn_partial_bytes, (cudaStream_t)stream);
     }
