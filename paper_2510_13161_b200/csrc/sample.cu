@@ -9,15 +9,16 @@
 // A cluster of CTAs has one row, each a contiguous part of it in shared memory (the logits leave HBM once), each warp a contiguous part of
 // that, so that sums in the order of the ids are sums over warps.
 //   1  load, maximum over the cluster
-//   2  a histogram of z in 2048 bins of 1/64: how many ids each holds, and, for Top-p, where in the bin they lie on average, which gives a
-//      bin's mass to 10^-4.  With Top-p over the whole row also the exact total
-//   3  the leading CTA reads off a bin that surely lies behind the end of the front
-//   4  if at most kList ids lie ahead of that, they all go to the leader, which sorts them and does the rest: the usual case
-//   4' otherwise only the bin in which the front ends goes to the leader, which sorts it; what lies ahead of it is counted and summed by all.
-//      (A bin of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
+//   2  a histogram of z in 2048 bins of 1/64: how many ids each holds and where in the bin they lie on average, packed in one word, which
+//      gives a bin's mass to 10^-3
+//   3  the leading CTA adds the histograms up and reads off the bin in which each filter's front ends, Top-p's by estimate
+//   4  if at most kList ids lie ahead of a bin that surely lies behind the end of the front, they go to the leader, in the order of their bins;
+//      it ranks those of a bin among themselves and does the rest.  Top-p's exact total is taken in the same pass
+//   4' otherwise only the bin in which the front ends goes to the leader; what lies ahead of it is counted and summed by all.  (A bin
+//      of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
 //   5  the drawn token, by the warps' masses, and the filtered distribution
 // What bounds it: double-precision arithmetic (18 operations an id, 64 a cycle and SM) where Top-p or a draw takes the whole row, the
-// bytes otherwise; for a row alone the cluster's barriers.
+// bytes otherwise; for a row alone the cluster's barriers and code that runs once.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -33,13 +34,17 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr float kBinsPerNat = 64.f;
-constexpr int kList = 2048;                   // candidates that the leader sorts
+constexpr int kList = 2048;                   // candidates that the leader ranks
+constexpr int kPer = kList / kThreads;
 constexpr int kMaxCluster = 16;
 constexpr int kMaxPart = 40960;               // ids of a CTA (160 KB)
+static_assert(kBins == kList, "a thread has as many bins as candidates");
 
 struct SampleParams {
     int V, M, part;                           // part: ids of a CTA, a multiple of 4 * kThreads
     int shift;                                // S
+    int id_shift;                             // ids >> id_shift are less than kList
+    int off_bits, off_shift;                  // of a histogram word: see pack_off
     int vec_in, vec_probs, vec_logits;        // rows begin on 16-byte boundaries
     float temperature;                        // of the ctx
     long long ld;
@@ -56,31 +61,38 @@ struct SampleParams {
     float* logits_out;
 };
 
+struct Sums {
+    u64 n, m, o, t;
+};
+struct Drawn {
+    u64 w;
+    uint32_t id, pad;
+};
+
 // What the CTAs of a cluster tell one another, and what a CTA's warps share.
 struct alignas(16) Shared {
     float max[kMaxCluster];
-    u64 sum[2][kMaxCluster][3];               // sums of the CTAs, for steps in turns
-    u64 warp_sum[kWarps][3];
+    u64 sum[2][kMaxCluster][4];               // sums of the CTAs, for steps in turns
+    u64 warp_sum[kWarps][4];
     u64 warp_mass[kWarps];                    // kept mass of the warps' parts
-    u64 total;                                // the row's mass
-    int last_bin, n_list, list_at;            // written by the leader
-    int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
     u64 cut_key;                              // composite key of the last kept id
     u64 kept;                                 // its front's mass
-    int drawn, n;
-    union {
-        struct {
-            uint32_t hist[kBins];
-            uint32_t off[kBins];
-        };
-        u64 list[kList];                      // (the histogram is no longer needed) composite keys: ~order key, id; ascending in rank
+    u64 base;
+    int last_bin, n_list, list_at;            // written by the leader
+    int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
+    int bucket;
+    float row_mass;
+    union alignas(16) {
+        uint32_t hist[kBins];                 // counts and offsets; the leader's: then where each bin's candidates go
+        Drawn drawn[kBins / 4];               // (the candidates that the draw has to look at one by one)
     };
-    u64 mass[kList];
+    u64 list[kList];                          // composite keys: ~order key, id; then the masses of buckets of ids
+    u64 ranked[kList];                        // the same in the order of the ranks
 };
-
 static_assert(sizeof(Shared) % 16 == 0, "the logits behind it are read 16 bytes at a time");
 
 __device__ __forceinline__ float unkey(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float logit_of(u64 key) { return unkey(~(uint32_t)(key >> 32)); }
 
 // round(2^S exp((l - max) / T)): y = (l - max) log2(e) / T = n + f with |f| <= 1/2, and 2^f by its Taylor series to f^11 (the next term
 // is below 7e-15).
@@ -133,26 +145,50 @@ __device__ __forceinline__ u64 warp_incl64(u64 v) {
     return v;
 }
 
-// The first n entries of the list in ascending order (bitonic, by the whole block).
-__device__ __noinline__ void sort_list(Shared& s, int n) {
+// list[0 .. n) ranked, by comparing all with all.
+__device__ __noinline__ void rank_list(Shared& s, int n) {
     const int tid = threadIdx.x;
-    int n2 = 32;
-    while (n2 < n) n2 <<= 1;
     __syncthreads();
-    for (int i = n + tid; i < n2; i += kThreads) s.list[i] = ~0ull;
-    for (int size = 2; size <= n2; size <<= 1)
-        for (int d = size >> 1; d; d >>= 1) {
-            __syncthreads();
-            for (int t = tid; t < n2 / 2; t += kThreads) {
-                const int i = ((t & ~(d - 1)) << 1) | (t & (d - 1)), j = i | d;
-                const u64 a = s.list[i], b = s.list[j];
-                if ((a > b) == ((i & size) == 0)) { s.list[i] = b; s.list[j] = a; }
-            }
+    u64 key[kPer];
+    int at[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        key[j] = tid + j * kThreads < n ? s.list[tid + j * kThreads] : ~0ull;
+        at[j] = 0;
+    }
+    const int rounds = (n + kThreads - 1) / kThreads;            // (elements of a thread that there are)
+#pragma unroll 4
+    for (int q = 0; q < n; ++q) {
+        const u64 k = s.list[q];
+        at[0] += k < key[0];
+        if (rounds > 1) {
+#pragma unroll
+            for (int j = 1; j < kPer; ++j) at[j] += k < key[j];
         }
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (tid + j * kThreads < n) s.ranked[at[j]] = key[j];
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant__ SampleParams p) {
+// A thread's w[], inclusive over the block: what lies before it, and all.
+__device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& before) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    u64 mine = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) mine += w[j];
+    const u64 in = warp_incl64(mine);
+    __syncthreads();
+    if (lane == 31) s.warp_sum[warp][0] = in;
+    __syncthreads();
+    u64 all = lane < kWarps ? s.warp_sum[lane][0] : 0ull;
+    all = warp_incl64(all);
+    before = in - mine + (warp ? __shfl_sync(0xffffffffu, all, warp - 1) : 0ull);
+    return __shfl_sync(0xffffffffu, all, kWarps - 1);
+}
+
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Shared& s = *reinterpret_cast<Shared*>(smem_raw);
     float* const z = reinterpret_cast<float*>(smem_raw + sizeof(Shared));
@@ -170,7 +206,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
     const float* const in = p.logits + (long long)row * p.ld + first;
     float mx = -INFINITY;
     if (p.vec_in) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = w0 + lane * 4; i < w1; i += 128) {
             float v[4];
             if (i + 4 <= n_mine) {
@@ -192,8 +228,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             z[i] = v;
         }
     }
-    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = s.off[i] = 0;
-    if (tid == 0) { s.n_list = 0; s.list_at = 0; }
+    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     if (lane == 0) s.warp_sum[warp][0] = __float_as_uint(mx);
@@ -219,6 +254,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
     const bool by_p = top_p < 1.0;
     const double min_p = p.min_p && !first_only ? (double)p.min_p[row] : 0.0;
     const bool by_m = min_p > 0.0;
+    const bool whole_total = by_p && !by_k;                      // Top-p of the whole row
     Weigh weigh;
     weigh.max = (double)mx;
     weigh.c = 1.4426950408889634074 / (double)T;
@@ -229,46 +265,52 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
     const u64 min_w = by_m ? (u64)fmin(ceil(min_p * exp2((double)p.shift)), exp2((double)p.shift)) : 0ull;
     // composite key of an id: smaller is ahead
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
-    int turn = 0;
-    // Sums over the cluster of what f(l, i, sums) adds for the ids of the part; every thread gets them.
-    struct Sums {
-        u64 n, m, o;
+    const float inv_T = 1.f / T;
+    auto bin_of = [&](float l, float& at) {
+        at = weigh.max_inf ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));
+        return (int)at;
     };
-    auto all_sums = [&](auto f) -> Sums {
-        Sums a = {0, 0, 0};
+    int turn = 0;
+    // a word of every CTA's for every CTA, by way of s.warp_sum
+    auto exchange = [&]() -> Sums {
+        __syncthreads();
+        if (tid < 4 * C) {
+            const int c = tid >> 2, q = tid & 3;
+            u64 t = 0;
+            for (int w = 0; w < kWarps; ++w) t += s.warp_sum[w][q];
+            cluster.map_shared_rank(&s, c)->sum[turn][rank][q] = t;
+        }
+        cluster.sync();
+        Sums a = {0, 0, 0, 0};
+        for (int c = 0; c < C; ++c) { a.n += s.sum[turn][c][0]; a.m += s.sum[turn][c][1]; a.o += s.sum[turn][c][2]; a.t += s.sum[turn][c][3]; }
+        turn ^= 1;                                               // (read before the other turn's barrier: rewritten after it)
+        return a;
+    };
+    // what f(l, i, sums) adds for the ids of the warp's part
+    auto warp_part = [&](auto f) -> Sums {
+        Sums a = {0, 0, 0, 0};
         for (int i = w0 + lane * 4; i < w1; i += 128) {
             const float4 v = *reinterpret_cast<const float4*>(z + i);
             f(v.x, i, a); f(v.y, i + 1, a); f(v.z, i + 2, a); f(v.w, i + 3, a);
         }
-        a.n = warp_sum64(a.n);
-        a.m = warp_sum64(a.m);
-        a.o = warp_sum64(a.o);
+        return {warp_sum64(a.n), warp_sum64(a.m), warp_sum64(a.o), warp_sum64(a.t)};
+    };
+    // ... summed over the cluster; every thread gets the sums
+    auto all_sums = [&](auto f) -> Sums {
+        const Sums a = warp_part(f);
         __syncthreads();
-        if (lane == 0) { s.warp_sum[warp][0] = a.n; s.warp_sum[warp][1] = a.m; s.warp_sum[warp][2] = a.o; }
-        __syncthreads();
-        if (tid < 3 * C) {
-            const int c = tid / 3, k = tid - c * 3;
-            u64 t = 0;
-            for (int w = 0; w < kWarps; ++w) t += s.warp_sum[w][k];
-            cluster.map_shared_rank(&s, c)->sum[turn][rank][k] = t;
-        }
-        cluster.sync();
-        a = {0, 0, 0};
-        for (int c = 0; c < C; ++c) { a.n += s.sum[turn][c][0]; a.m += s.sum[turn][c][1]; a.o += s.sum[turn][c][2]; }
-        turn ^= 1;                                               // (read before the other turn's barrier: rewritten after it)
-        return a;
+        if (lane == 0) { s.warp_sum[warp][0] = a.n; s.warp_sum[warp][1] = a.m; s.warp_sum[warp][2] = a.o; s.warp_sum[warp][3] = a.t; }
+        return exchange();
     };
 
     u64 cut = ~0ull;                                             // composite key of the last id of the front
-    u64 total = 0;
+    bool listed = false;
+    int ahead_bin = -1;                                          // >= 0: the warps' masses ahead of that bin are in s.warp_mass, with their counts
+    u64 Z = 0;
     if (!none && (by_k || by_p || by_m)) {
-        // ---- 2: histogram
-        const float inv_T = 1.f / T;
-        auto bin_of = [&](float l, float& at) {
-            at = weigh.max_inf ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));
-            return (int)at;
-        };
-        const bool whole_total = by_p && !by_k;                  // Top-p of the whole row
+        // ---- 2: histogram.  A word counts in its upper bits and sums in its lower ones in which part of the bin the ids lie: neither half
+        // outgrows its bits over a part's ids.
+        const float parts = (float)(1 << p.off_bits);
         for (int i = w0 + lane * 4; i < w1; i += 128) {
             const float4 v4 = *reinterpret_cast<const float4*>(z + i);
             const float v[4] = {v4.x, v4.y, v4.z, v4.w};
@@ -277,113 +319,101 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 if (!may(v[j])) continue;
                 float at;
                 const int bin = bin_of(v[j], at);
-                atomicAdd(&s.hist[bin], 1u);
-                if (by_p) atomicAdd(&s.off[bin], (uint32_t)((at - (float)bin) * 1024.f));
-                if (whole_total) total += weigh(v[j]);
+                atomicAdd(&s.hist[bin], (1u << p.off_shift) + (uint32_t)((at - (float)bin) * parts));
             }
         }
-        total = warp_sum64(total);
-        if (lane == 0) s.warp_sum[warp][0] = total;
-        __syncthreads();
-        if (tid == 0) {
-            u64 a = 0;
-            for (int w = 0; w < kWarps; ++w) a += s.warp_sum[w][0];
-            lead->sum[0][rank][0] = a;
-        }
-        if (rank != 0)
-            for (int i = tid; i < kBins; i += kThreads) {
-                const uint32_t n = s.hist[i];
-                if (n) {
-                    atomicAdd(&lead->hist[i], n);
-                    if (by_p) atomicAdd(&lead->off[i], s.off[i]);
-                }
-            }
         cluster.sync();
-        // ---- 3: a bin behind the front's end
+        // ---- 3: the bins in which the fronts end
         if (rank == 0) {
-            constexpr int kPer = kBins / kThreads;
-            u64 n = 0;
-            double m = 0.0;
-            uint32_t cnt[kPer];
-            double ms[kPer];
+            uint32_t cnt[kPer] = {}, off[kPer] = {};
+            const uint32_t low = (1u << p.off_shift) - 1u;
+#pragma unroll 4
+            for (int c = 0; c < C; ++c) {
+                const uint4 h = *reinterpret_cast<const uint4*>(&cluster.map_shared_rank(&s, c)->hist[tid * kPer]);
+                cnt[0] += h.x >> p.off_shift; cnt[1] += h.y >> p.off_shift; cnt[2] += h.z >> p.off_shift; cnt[3] += h.w >> p.off_shift;
+                off[0] += h.x & low; off[1] += h.y & low; off[2] += h.z & low; off[3] += h.w & low;
+            }
+            uint32_t n = 0;
+            float m = 0.f, ms[kPer];
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
+                // (the mean of exp(-x) over a 64th is exp(-mean) but for a relative 10^-4; the last bin is open: no mass)
                 const int b = tid * kPer + j;
-                cnt[j] = s.hist[b];
-                ms[j] = 0.0;
-                if (cnt[j] && by_p) {
-                    // (the mean of exp(-x) over a 64th is exp(-mean) but for a relative x^2 / 2 of 10^-4; the last bin is open: no mass)
-                    const float mean = ((float)b + (float)s.off[b] * (1.f / 1024.f) / (float)cnt[j]) * (1.f / kBinsPerNat);
-                    ms[j] = b == kBins - 1 ? 0.0 : (double)cnt[j] * (double)expf(-mean);
-                }
+                const float mean = ((float)b + __fdividef((float)off[j] + 0.5f * (float)cnt[j], parts * fmaxf((float)cnt[j], 1.f))) * (1.f / kBinsPerNat);
+                ms[j] = b == kBins - 1 ? 0.f : (float)cnt[j] * __expf(-mean);
                 n += cnt[j];
                 m += ms[j];
             }
             // exclusive sums over the threads
-            u64 n_in = warp_incl64(n);
-            double m_in = m;
+            uint32_t n_in = n;
+            float m_in = m;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const double t = __shfl_up_sync(0xffffffffu, m_in, o);
-                if (lane >= o) m_in += t;
+                const uint32_t a = __shfl_up_sync(0xffffffffu, n_in, o);
+                const float b = __shfl_up_sync(0xffffffffu, m_in, o);
+                if (lane >= o) { n_in += a; m_in += b; }
             }
-            if (lane == 31) { s.warp_sum[warp][0] = n_in; s.warp_sum[warp][1] = (u64)__double_as_longlong(m_in); }
+            if (lane == 31) s.warp_sum[warp][0] = ((u64)n_in << 32) | __float_as_uint(m_in);
             if (tid == 0) {
                 s.last_bin = s.bin_k = s.bin_p = kBins - 1;
-                u64 a = 0;
-                for (int c = 0; c < C; ++c) a += s.sum[0][c][0];
-                s.total = a;
+                s.list_at = 0;
             }
             __syncthreads();
-            for (int w = 0; w < warp; ++w) { n_in += s.warp_sum[w][0]; m_in += __longlong_as_double((long long)s.warp_sum[w][1]); }
-            u64 nb = n_in - n;
-            double mb = m_in - m;
+            float m_all = 0.f;
+            uint32_t n_before = n_in - n;
+            float m_before = m_in - m;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const u64 t = s.warp_sum[w][0];
+                if (w < warp) { n_before += (uint32_t)(t >> 32); m_before += __uint_as_float((uint32_t)t); }
+                m_all += __uint_as_float((uint32_t)t);
+            }
+            if (tid == 0) s.row_mass = m_all;
+            __syncthreads();
             // Top-k's bin, and about what its front weighs
             if (by_k) {
+                uint32_t nb = n_before;
+                float mb = m_before;
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
-                    if (nb < (u64)k && nb + cnt[j] >= (u64)k) {
+                    if (nb < (uint32_t)k && nb + cnt[j] >= (uint32_t)k) {
                         s.bin_k = tid * kPer + j;
-                        s.warp_mass[0] = (u64)__double_as_longlong(mb + ms[j] * (double)(k - (int)nb) / (double)cnt[j]);
+                        s.row_mass = mb + ms[j] * (float)((uint32_t)k - nb) / (float)cnt[j];
                     }
                     nb += cnt[j];
                     mb += ms[j];
                 }
-                if (tid == kThreads - 1 && nb < (u64)k) s.warp_mass[0] = (u64)__double_as_longlong(mb);
                 __syncthreads();
-                nb = n_in - n;
-                mb = m_in - m;
             }
-            const double row_mass = by_k ? __longlong_as_double((long long)s.warp_mass[0]) : (double)s.total * exp2(-(double)p.shift);
-            const double about = by_p ? top_p * row_mass : 0.0, want = whole_total ? about * 1.002 : 0.0;
-            // (Top-p behind Top-k is a share of all that Top-k leaves: then Min-p does not shorten the list)
-            const float m_at = -logf((float)fmin(min_p, 1.0)) * kBinsPerNat + 1.f;
-            const bool m_ends = by_m && !(by_k && by_p);
+            // (Top-p behind Top-k is a share of all that Top-k leaves: then nothing else shortens the list)
+            const float about = (float)top_p * s.row_mass, m_at = -logf((float)fmin(min_p, 1.0)) * kBinsPerNat + 1.f;
+            const bool p_ends = whole_total, m_ends = by_m && !(by_k && by_p);
+            uint32_t nb = n_before;
+            float mb = m_before;
+            int end = kBins - 1, end_p = kBins - 1;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
+                const int b = tid * kPer + j;
                 nb += cnt[j];
                 mb += ms[j];
                 // the first bin at which one of the filters is surely through
-                if ((by_k && nb >= (u64)k) || (whole_total && mb >= want) || (m_ends && (float)(tid * kPer + j) >= m_at)) {
-                    atomicMin(&s.last_bin, tid * kPer + j);
-                    break;
-                }
+                if ((by_k && nb >= (uint32_t)k) || (p_ends && mb >= 1.01f * about) || (m_ends && (float)b >= m_at)) end = min(end, b);
+                if (by_p && mb >= about) end_p = min(end_p, b);
             }
-            mb = m_in - m;
-            if (by_p) {
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    mb += ms[j];
-                    if (mb >= about) { atomicMin(&s.bin_p, tid * kPer + j); break; }
-                }
+            end = __reduce_min_sync(0xffffffffu, end);
+            end_p = __reduce_min_sync(0xffffffffu, end_p);
+            if (lane == 0) {
+                atomicMin(&s.last_bin, end);
+                atomicMin(&s.bin_p, end_p);
             }
             __syncthreads();
-            // how many ids that is
-            nb = n_in - n;
+            // how many ids that is, and where each bin's go
+            nb = n_before;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
+                s.hist[tid * kPer + j] = nb;
                 nb += cnt[j];
-                if (tid * kPer + j == s.last_bin) s.n_list = (int)min(nb, (u64)0x7fffffff);
+                if (tid * kPer + j == s.last_bin) s.n_list = (int)nb;
             }
             __syncthreads();
             if (tid < C) {
@@ -392,58 +422,47 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 o->bin_k = s.bin_k;
                 o->bin_p = s.bin_p;
                 o->n_list = s.n_list;
-                o->total = s.total;
             }
         }
         cluster.sync();
         const int n_list = s.n_list, last_bin = s.last_bin;
-        total = s.total;
-        if (n_list <= kList) {
-            // ---- 4: the leader's list
-            for (int i = w0 + lane * 4; i < w1; i += 128) {
-                const float4 v4 = *reinterpret_cast<const float4*>(z + i);
-                const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (!may(v[j])) continue;
-                    float at;
-                    if (bin_of(v[j], at) > last_bin) continue;
-                    const int slot = atomicAdd(&lead->list_at, 1);
-                    if (slot < kList) lead->list[slot] = key_of(v[j], first + i + j);
-                }
-            }
-            cluster.sync();
+        listed = n_list <= kList;
+        if (listed) {
+            // ---- 4: the leader's list, and Top-p's total
+            const Sums a = warp_part([&](float l, int i, Sums& a) {
+                if (!may(l)) return;
+                if (whole_total) a.m += weigh(l);
+                float at;
+                const int bin = bin_of(l, at);
+                if (bin > last_bin) return;
+                const uint32_t slot = atomicAdd(&lead->hist[bin], 1u);
+                if (slot < (uint32_t)kList) lead->list[slot] = key_of(l, first + i);
+            });
+            __syncthreads();
+            if (lane == 0) { s.warp_sum[warp][0] = s.warp_sum[warp][2] = s.warp_sum[warp][3] = 0; s.warp_sum[warp][1] = a.m; }
+            const u64 total = exchange().m;
             if (rank == 0) {
-                sort_list(s, n_list);
-                constexpr int kPer = kList / kThreads;
-                // inclusive sums of mass[] over the list: a thread has neighbours
-                auto scan = [&](u64 (&w)[kPer], u64& before) -> u64 {
-                    u64 mine = 0;
+                // ranks: the bin's place, and the place within the bin
 #pragma unroll
-                    for (int j = 0; j < kPer; ++j) mine += w[j];
-                    const u64 in_ = warp_incl64(mine);
-                    __syncthreads();
-                    if (lane == 31) s.warp_sum[warp][0] = in_;
-                    __syncthreads();
-                    before = in_ - mine;
-                    u64 all = 0;
-                    for (int q = 0; q < kWarps; ++q) {
-                        if (q < warp) before += s.warp_sum[q][0];
-                        all += s.warp_sum[q][0];
-                    }
-                    return all;
-                };
-                u64 w[kPer], before;
+                for (int j = 0; j < kPer; ++j) {
+                    const int r = tid + j * kThreads;
+                    if (r >= n_list) break;
+                    const u64 key = s.list[r];
+                    float at;
+                    const int bin = bin_of(logit_of(key), at), lo = bin ? (int)s.hist[bin - 1] : 0, hi = (int)s.hist[bin];
+                    int ahead = 0;
+                    for (int q = lo; q < hi; ++q) ahead += s.list[q] < key;
+                    s.ranked[lo + ahead] = key;
+                }
+                __syncthreads();
+                u64 w[kPer], sel[kPer], before;
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
                     const int r = tid * kPer + j;
-                    w[j] = r < n_list ? weigh(unkey(~(uint32_t)(s.list[r] >> 32))) : 0ull;
-                    if (r < n_list) s.mass[r] = w[j];
+                    w[j] = r < n_list ? weigh(logit_of(s.ranked[r])) : 0ull;
+                    sel[j] = by_k && r >= k ? 0ull : w[j];
                 }
-                u64 sel[kPer];
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) sel[j] = by_k && tid * kPer + j >= k ? 0ull : w[j];
-                const u64 part = scan(sel, before);
+                const u64 part = block_scan(s, sel, before);
                 const double want = top_p * (double)(whole_total ? total : part);
                 int kept = 0;
                 u64 kept_mass = 0;
@@ -457,54 +476,62 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 }
                 kept = __reduce_add_sync(0xffffffffu, kept);
                 kept_mass = warp_sum64(kept_mass);
-                __syncthreads();
-                if (lane == 0) { s.warp_sum[warp][0] = (u64)kept; s.warp_sum[warp][1] = kept_mass; }
+                if (lane == 0) { s.warp_sum[warp][2] = (u64)kept; s.warp_sum[warp][3] = kept_mass; }
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) s.list[tid * kPer + j] = 0;           // (from here on: masses of buckets of ids)
+                if (tid == 0) s.list_at = 0;
                 __syncthreads();
                 int n = 0;
-                u64 Z = 0;
-                for (int q = 0; q < kWarps; ++q) { n += (int)s.warp_sum[q][0]; Z += s.warp_sum[q][1]; }
-                const u64 last = s.list[n - 1];
+                Z = 0;
+#pragma unroll
+                for (int q = 0; q < kWarps; ++q) { n += (int)s.warp_sum[q][2]; Z += s.warp_sum[q][3]; }
                 if (tid < C && (p.probs || p.logits_out)) {
                     Shared* const o = cluster.map_shared_rank(&s, tid);
-                    o->cut_key = last;
+                    o->cut_key = s.ranked[n - 1];
                     o->kept = Z;
                 }
-                // the draw: the kept ids in their own order (id, then the key's place in the list)
+                // the draw: the bucket of ids in which the sum over ids passes the uniform's share, then the id within it
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (tid * kPer + j < n) atomicAdd(&s.list[(uint32_t)s.ranked[tid * kPer + j] >> p.id_shift], w[j]);
                 __syncthreads();
-                u64 by_id[kPer];
+                u64 bucket[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) bucket[j] = s.list[tid * kPer + j];
+                block_scan(s, bucket, before);
+                const double t = fmax((double)p.u[row], 0.0) * (double)Z;
+                const u64 target = t >= (double)Z ? Z - 1 : (u64)t;                 // the first id whose inclusive sum is above it
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
-                    const int r = tid + j * kThreads;
-                    by_id[j] = r < n ? ((s.list[r] & 0xffffffffull) << 32) | (uint32_t)r : ~0ull;
+                    if (before <= target && before + bucket[j] > target) {
+                        s.bucket = tid * kPer + j;
+                        s.base = before;
+                    }
+                    before += bucket[j];
                 }
                 __syncthreads();
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) s.list[tid + j * kThreads] = by_id[j];
-                sort_list(s, n);
-#pragma unroll
                 for (int j = 0; j < kPer; ++j) {
-                    const int r = tid * kPer + j;
-                    w[j] = r < n ? s.mass[(uint32_t)s.list[r]] : 0ull;
+                    const uint32_t id = (uint32_t)s.ranked[tid * kPer + j];
+                    if (tid * kPer + j < n && (int)(id >> p.id_shift) == s.bucket) s.drawn[atomicAdd(&s.list_at, 1)] = {w[j], id, 0u};
                 }
-                scan(w, before);
-                const float u = p.u[row];
-                const double t = fmax((double)u, 0.0) * (double)Z;
-                const u64 target = t >= (double)Z ? Z - 1 : (u64)t;          // the first id whose inclusive sum is above it
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const int r = tid * kPer + j;
-                    if (r < n && before <= target && before + w[j] > target) {
-                        p.token[row] = (int32_t)(s.list[r] >> 32);
-                        if (p.logprob) p.logprob[row] = (float)log((double)w[j] / (double)Z);
+                __syncthreads();
+                for (int q = tid; q < s.list_at; q += kThreads) {
+                    const Drawn d = s.drawn[q];
+                    u64 sum = s.base;
+                    for (int q2 = 0; q2 < s.list_at; ++q2)
+                        if (s.drawn[q2].id < d.id) sum += s.drawn[q2].w;
+                    if (sum <= target && sum + d.w > target) {
+                        p.token[row] = (int32_t)d.id;
+                        if (p.logprob) p.logprob[row] = (float)log((double)d.w / (double)Z);
                         if (p.n_kept) p.n_kept[row] = n;
                     }
-                    before += w[j];
                 }
             }
             if (!p.probs && !p.logits_out) return;
             cluster.sync();
             cut = s.cut_key;
-            total = s.kept;
+            Z = s.kept;
         } else {
             // ---- 4': the bin in which each filter's front ends, and where in it
             auto front = [&](u64 at) {                           // (count, mass) of the ids up to the composite key `at`
@@ -522,84 +549,98 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                 }
                 return lo;
             };
-            // The smallest key whose front (count, mass) fulfils `done`, which is monotone; guessed to lie in bin `b`.
-            auto end_of = [&](int b, bool by_mass, auto done) -> u64 {
-                u64 n0, m0, n_in;
-                for (;;) {
+            // The smallest key whose front (count, mass, and the mass of all ids where that is asked for) fulfils `done`, which is monotone;
+            // guessed to lie in bin `b`.
+            auto end_of = [&](int b, bool by_mass, bool of_all, auto done) -> u64 {
+                u64 n0, m0, n_in, all = 0;
+                u64 lo = 0, hi = ~0ull;                          // (what is known of the key where the guess is off again and again)
+                bool far = false;
+                for (int again = 0;; ++again) {
                     // what lies ahead of the bin, and the bin itself into the leader's list
                     if (rank == 0 && tid == 0) s.list_at = 0;
                     cluster.sync();
-                    const Sums a = all_sums([&](float l, int i, Sums& a) {
+                    const bool rest = of_all && again == 0;
+                    const Sums mine = warp_part([&](float l, int i, Sums& a) {
                         if (!may(l)) return;
                         float at;
                         const int bin = bin_of(l, at);
-                        if (bin > b) return;
+                        if (bin > b && !rest) return;
                         const u64 w = by_mass ? weigh(l) : 0ull;
                         if (bin < b) {
                             ++a.n;
                             a.m += w;
-                        } else {
+                        } else if (bin == b) {
                             a.n += 1ull << 32;
                             a.o += w;
                             const int slot = atomicAdd(&lead->list_at, 1);
                             if (slot < kList) lead->list[slot] = key_of(l, first + i);
+                        } else {
+                            a.t += w;
                         }
                     });
+                    __syncthreads();
+                    if (lane == 0) {
+                        s.warp_sum[warp][0] = mine.n; s.warp_sum[warp][1] = mine.m; s.warp_sum[warp][2] = mine.o; s.warp_sum[warp][3] = mine.t;
+                        s.warp_mass[warp] = mine.m;
+                    }
+                    const Sums a = exchange();
                     n0 = a.n & 0xffffffffull;
                     n_in = a.n >> 32;
                     m0 = a.m;
-                    if (n0 > 0 && done(n0, m0)) { --b; continue; }                                // it ends ahead of this bin
-                    if (b < kBins - 1 && !done(n0 + n_in, m0 + a.o)) { ++b; continue; }           // ... or behind it
-                    break;
+                    if (rest) all = a.m + a.o + a.t;
+                    ahead_bin = by_mass ? b : -1;
+                    const bool early = n0 > 0 && done(n0, m0, all), late = b < kBins - 1 && !done(n0 + n_in, m0 + a.o, all);
+                    far = (early || late) && again >= 3;
+                    // (the bin's own keys, or all ahead of it, or all behind it)
+                    if (far || n_in > (u64)kList) {
+                        lo = early || b == 0 ? 0ull : (u64)~(edge(b - 1) - 1) << 32;
+                        hi = late ? ~0ull : ((u64)~edge(b) << 32) | 0xffffffffull;
+                    }
+                    if (far || !(early || late)) break;
+                    b += early ? -1 : 1;                         // it ends ahead of this bin, or behind it
                 }
-                if (n_in > (u64)kList) {
-                    u64 lo = b > 0 ? (u64)~(edge(b - 1) - 1) << 32 : 0ull, hi = ((u64)~edge(b) << 32) | 0xffffffffull;
+                if (far) ahead_bin = -1;
+                if (far || n_in > (u64)kList) {
                     while (lo < hi) {
                         const u64 mid = lo + ((hi - lo) >> 1);
                         const Sums a = front(mid);
-                        if (done(a.n, a.m)) hi = mid; else lo = mid + 1;
+                        if (done(a.n, a.m, all)) hi = mid; else lo = mid + 1;
                     }
                     return lo;
                 }
                 if (rank == 0) {
                     const int n = (int)n_in;
-                    sort_list(s, n);
-                    constexpr int kPer = kList / kThreads;
-                    u64 w[kPer], mine = 0;
+                    rank_list(s, n);
+                    if (tid == 0) s.list_at = n - 1;
+                    u64 w[kPer], at;
 #pragma unroll
                     for (int j = 0; j < kPer; ++j) {
                         const int r = tid * kPer + j;
-                        w[j] = by_mass && r < n ? weigh(unkey(~(uint32_t)(s.list[r] >> 32))) : 0ull;
-                        mine += w[j];
+                        w[j] = by_mass && r < n ? weigh(logit_of(s.ranked[r])) : 0ull;
                     }
-                    u64 at = warp_incl64(mine);
-                    __syncthreads();
-                    if (lane == 31) s.warp_sum[warp][0] = at;
-                    if (tid == 0) s.list_at = n - 1;
-                    __syncthreads();
-                    at += m0 - mine;
-                    for (int q = 0; q < warp; ++q) at += s.warp_sum[q][0];
+                    block_scan(s, w, at);
+                    at += m0;
 #pragma unroll
                     for (int j = 0; j < kPer; ++j) {
                         const int r = tid * kPer + j;
                         at += w[j];
-                        if (r < n && done(n0 + r + 1, at)) { atomicMin(&s.list_at, r); break; }
+                        if (r < n && done(n0 + r + 1, at, all)) { atomicMin(&s.list_at, r); break; }
                     }
                     __syncthreads();
-                    if (tid < C) cluster.map_shared_rank(&s, tid)->cut_key = s.list[s.list_at];
+                    if (tid < C) cluster.map_shared_rank(&s, tid)->cut_key = s.ranked[s.list_at];
                 }
                 cluster.sync();
                 const u64 c = s.cut_key;
                 cluster.sync();                                  // (the next one may be written)
                 return c;
             };
+            u64 total = 0;
             if (by_k) {
-                cut = end_of(s.bin_k, false, [&](u64 n, u64) { return n >= (u64)k; });
+                cut = end_of(s.bin_k, false, false, [&](u64 n, u64, u64) { return n >= (u64)k; });
                 if (by_p) total = front(cut).m;
             }
             if (by_p) {
-                const double want = top_p * (double)total;
-                const u64 c = end_of(s.bin_p, true, [&](u64 n, u64 m) { return n >= 1 && (double)m >= want; });
+                const u64 c = end_of(s.bin_p, true, whole_total, [&](u64 n, u64 m, u64 all) { return n >= 1 && (double)m >= top_p * (double)(whole_total ? all : total); });
                 cut = min(cut, c);
             }
             if (by_m) {
@@ -612,69 +653,69 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
                         const float l = unkey(mid);
                         if (l > -INFINITY && weigh(l) >= min_w) hi = mid; else lo = mid + 1;
                     }
-                    if (lane == 0) s.warp_mass[0] = ((u64)~hi << 32) | 0xffffffffull;
+                    if (lane == 0) s.base = ((u64)~hi << 32) | 0xffffffffull;
                 }
                 __syncthreads();
-                cut = min(cut, s.warp_mass[0]);
-                __syncthreads();
+                if (s.base < cut) { cut = s.base; ahead_bin = -1; }
             }
         }
     }
     // ---- 5: the warps' kept masses, the draw, the distribution
     auto kept = [&](float l, int i) { return may(l) && key_of(l, first + i) <= cut; };
-    const bool listed = !none && (by_k || by_p || by_m) && s.n_list <= kList;
-    u64 Z = total;
     if (!listed) {
-        u64 n = 0, m = 0;
-        for (int i = w0 + lane * 4; i < w1; i += 128) {
-            const float4 v4 = *reinterpret_cast<const float4*>(z + i);
-            const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (kept(v[j], i + j)) { ++n; m += weigh(v[j]); }
-        }
-        n = warp_sum64(n);
-        m = warp_sum64(m);
+        // (ahead of the bin in which the front ends the masses are known)
+        const Sums mine = warp_part([&](float l, int i, Sums& a) {
+            if (!kept(l, i)) return;
+            ++a.n;
+            float at;
+            if (ahead_bin < 0 || bin_of(l, at) >= ahead_bin) a.m += weigh(l);
+        });
+        const u64 mass = mine.m + (ahead_bin < 0 ? 0ull : s.warp_mass[warp]);
         __syncthreads();
-        if (lane == 0) { s.warp_sum[warp][0] = n; s.warp_mass[warp] = m; }
-        __syncthreads();
-        if (tid < C) {
-            u64 a = 0, b = 0;
-            for (int w = 0; w < kWarps; ++w) { a += s.warp_sum[w][0]; b += s.warp_mass[w]; }
-            Shared* const o = cluster.map_shared_rank(&s, tid);
-            o->sum[turn][rank][0] = a;
-            o->sum[turn][rank][1] = b;
+        if (lane == 0) {
+            s.warp_sum[warp][0] = mine.n; s.warp_sum[warp][1] = mass; s.warp_sum[warp][2] = s.warp_sum[warp][3] = 0;
+            s.warp_mass[warp] = mass;
         }
-        cluster.sync();
-        n = 0;
-        Z = 0;
-        u64 before = 0;                                          // mass of the CTAs ahead
-        for (int c = 0; c < C; ++c) {
-            n += s.sum[turn][c][0];
-            if (c < rank) before += s.sum[turn][c][1];
-            Z += s.sum[turn][c][1];
-        }
-        if (n == 0) {
+        const int was = turn;
+        const Sums all = exchange();
+        Z = all.m;
+        if (all.n == 0) {
             if (rank == 0 && tid == 0) {
                 p.token[row] = -1;
                 if (p.logprob) p.logprob[row] = -INFINITY;
                 if (p.n_kept) p.n_kept[row] = 0;
             }
         } else {
-            if (rank == 0 && tid == 0 && p.n_kept) p.n_kept[row] = (int32_t)n;
+            if (rank == 0 && tid == 0 && p.n_kept) p.n_kept[row] = (int32_t)all.n;
             const double t = fmax((double)p.u[row], 0.0) * (double)Z;
             const u64 target = t >= (double)Z ? Z - 1 : (u64)t;
+            u64 before = 0;
+            for (int c = 0; c < rank; ++c) before += s.sum[was][c][1];
             for (int w = 0; w < warp; ++w) before += s.warp_mass[w];
-            if (before <= target && before + s.warp_mass[warp] > target) {
-                for (int i0 = w0; i0 < w1; i0 += 32) {           // (this warp's ids in order)
-                    const int i = i0 + lane;
-                    const float l = i < w1 ? z[i] : -INFINITY;
-                    const u64 w = i < w1 && kept(l, i) ? weigh(l) : 0ull, in_ = before + warp_incl64(w);
+            if (before <= target && before + mass > target) {
+                for (int i0 = w0; i0 < w1; i0 += 128) {          // (this warp's ids in order, four to a lane)
+                    const int i = i0 + lane * 4;
+                    u64 w[4] = {};
+                    if (i < w1) {
+                        const float4 v4 = *reinterpret_cast<const float4*>(z + i);
+                        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (kept(v[j], i + j)) w[j] = weigh(v[j]);
+                    }
+                    const u64 four = w[0] + w[1] + w[2] + w[3], in_ = before + warp_incl64(four);
                     const uint32_t over = __ballot_sync(0xffffffffu, in_ > target);
                     if (over) {
                         if (lane == __ffs(over) - 1) {
-                            p.token[row] = first + i;
-                            if (p.logprob) p.logprob[row] = (float)log((double)w / (double)Z);
+                            u64 at = in_ - four;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (at <= target && at + w[j] > target) {
+                                    p.token[row] = first + i + j;
+                                    if (p.logprob) p.logprob[row] = (float)log((double)w[j] / (double)Z);
+                                }
+                                at += w[j];
+                            }
                         }
                         break;
                     }
@@ -696,7 +737,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const __grid_constant_
             for (int j = 0; j < 4; ++j) {
                 const bool in_front = kept(v[j], i + j);
                 a[j] = in_front && probs ? (float)(weigh.exact(v[j]) * inv) : 0.f;
-                b[j] = in_front ? (float)(weigh.y_of(v[j]) * ln2T - ln_z * (double)p.temperature) : -INFINITY;
+                b[j] = in_front && lg ? (float)(weigh.y_of(v[j]) * ln2T - ln_z * (double)p.temperature) : -INFINITY;
             }
             const bool whole = i + 4 <= n_mine;
             if (probs) {
@@ -741,6 +782,7 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     int bits = 0;
     while ((1ll << bits) < V) ++bits;
     p.shift = 62 - bits < 51 ? 62 - bits : 51;                   // (a weight has to fit a double's 52 bits)
+    p.id_shift = bits > 11 ? bits - 11 : 0;
     p.temperature = ctx->temperature;
     p.logits = logits; p.temperatures = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.u = u;
     p.token = token; p.logprob = logprob; p.n_kept = n_kept; p.probs = probs; p.logits_out = logits_out;
@@ -752,6 +794,9 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     auto part = [&](int c) { return (int)(align_up((size_t)((V + c - 1) / c), 4 * kThreads)); };
     while (C < kMaxCluster && (part(C) > 16384 || (part(C) > 4 * kThreads && (int64_t)2 * C * M <= ctx->num_sms))) C <<= 1;
     p.part = part(C);
+    // a histogram word: up to `part` ids counted above, their places of three bits (or one) summed below
+    p.off_bits = p.part <= 16384 ? 3 : 1;
+    p.off_shift = p.part <= 16384 ? 17 : 16;
     const size_t smem = sizeof(Shared) + (size_t)p.part * sizeof(float);
     MIRROR_CUDA_OK(cudaFuncSetAttribute(sample_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (C > 8) MIRROR_CUDA_OK(cudaFuncSetAttribute(sample_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
