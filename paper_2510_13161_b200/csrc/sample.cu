@@ -6,9 +6,11 @@
 // share is 10^-5 where the row is open).  Weights are therefore 64-bit integers, round(exp(z) 2^S) with S = 62 - ceil(log2 V), from a
 // double-precision exponential: their sums are exact, and the same in whatever order threads and CTAs take them.
 //
-// A cluster of CTAs has one row, each a contiguous part of it in shared memory (the logits leave HBM once), each warp a contiguous part of
-// that, so that sums in the order of the ids are sums over warps.
-//   1  load, maximum over the cluster
+// A cluster of CTAs has one row, each a contiguous part of it, each warp a contiguous part of that, so that sums in the order of the ids
+// are sums over warps.  With few rows a part is kept in shared memory.  With many it is read again from L2 by every pass: what takes
+// the time then is the steps that one CTA, or one thread, takes for its row while the others wait, so four small CTAs an SM, each with
+// more of a row, get more rows through than two large ones (520 rows: 541 -> MEASURED us).
+//   1  load, maximum over the cluster (the logits leave HBM once)
 //   2  a histogram of z in 2048 bins of 1/64: how many ids each holds and where in the bin they lie on average, packed in one word, which
 //      gives a bin's mass to 10^-3
 //   3  the leading CTA adds the histograms up and reads off the bin in which each filter's front ends, Top-p's by estimate
@@ -30,18 +32,16 @@ namespace {
 
 using u64 = unsigned long long;
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
+constexpr int kMaxWarps = 16;                 // 512 threads a CTA, or 256
 constexpr int kBins = 2048;
 constexpr float kBinsPerNat = 64.f;
 constexpr int kList = 2048;                   // candidates that the leader ranks
-constexpr int kPer = kList / kThreads;
 constexpr int kMaxCluster = 16;
-constexpr int kMaxPart = 40960;               // ids of a CTA (160 KB)
+constexpr int kMaxPart = 40960;               // ids of a CTA
 static_assert(kBins == kList, "a thread has as many bins as candidates");
 
 struct SampleParams {
-    int V, M, part;                           // part: ids of a CTA, a multiple of 4 * kThreads
+    int V, M, part;                           // part: ids of a CTA, a multiple of 128 per warp
     int shift;                                // S
     int id_shift;                             // ids >> id_shift are less than kList
     int off_bits, off_shift;                  // of a histogram word: see pack_off
@@ -73,8 +73,8 @@ struct Drawn {
 struct alignas(16) Shared {
     float max[kMaxCluster];
     u64 sum[2][kMaxCluster][4];               // sums of the CTAs, for steps in turns
-    u64 warp_sum[kWarps][4];
-    u64 warp_mass[kWarps];                    // kept mass of the warps' parts
+    u64 warp_sum[kMaxWarps][4];
+    u64 warp_mass[kMaxWarps];                    // kept mass of the warps' parts
     u64 cut_key;                              // composite key of the last kept id
     u64 kept;                                 // its front's mass
     u64 base;
@@ -146,7 +146,9 @@ __device__ __forceinline__ u64 warp_incl64(u64 v) {
 }
 
 // list[0 .. n) ranked, by comparing all with all.
+template <int kThreads>
 __device__ __noinline__ void rank_list(Shared& s, int n) {
+    constexpr int kPer = kList / kThreads;
     const int tid = threadIdx.x;
     __syncthreads();
     u64 key[kPer];
@@ -173,7 +175,9 @@ __device__ __noinline__ void rank_list(Shared& s, int n) {
 }
 
 // A thread's w[], inclusive over the block: what lies before it, and all.
+template <int kPer>
 __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& before) {
+    constexpr int kWarps = kList / kPer / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     u64 mine = 0;
 #pragma unroll
@@ -188,10 +192,12 @@ __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& 
     return __shfl_sync(0xffffffffu, all, kWarps - 1);
 }
 
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
+template <bool kResident, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const __grid_constant__ SampleParams p) {
+    constexpr int kWarps = kThreads / 32, kPer = kList / kThreads;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Shared& s = *reinterpret_cast<Shared*>(smem_raw);
-    float* const z = reinterpret_cast<float*>(smem_raw + sizeof(Shared));
+    float* const z = reinterpret_cast<float*>(smem_raw + sizeof(Shared));         // (resident)
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), row = blockIdx.x / C;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -205,29 +211,25 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     // ---- 1: load, maximum.  (What cannot be kept, NaN and the part's end, becomes -inf.)
     const float* const in = p.logits + (long long)row * p.ld + first;
     float mx = -INFINITY;
-    if (p.vec_in) {
-#pragma unroll 8
-        for (int i = w0 + lane * 4; i < w1; i += 128) {
-            float v[4];
-            if (i + 4 <= n_mine) {
-                *reinterpret_cast<float4*>(v) = __ldcs(reinterpret_cast<const float4*>(in + i));
-            } else {
+    auto fetch = [&](int i) -> float4 {                          // four ids' logits from memory
+        float v[4];
+        if (p.vec_in && i + 4 <= n_mine) {
+            *reinterpret_cast<float4*>(v) = kResident ? __ldcs(reinterpret_cast<const float4*>(in + i)) : *reinterpret_cast<const float4*>(in + i);
+        } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = i + j < n_mine ? in[i + j] : -INFINITY;
-            }
+            for (int j = 0; j < 4; ++j) v[j] = i + j < n_mine ? in[i + j] : -INFINITY;
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { v[j] = v[j] == v[j] ? v[j] : -INFINITY; mx = fmaxf(mx, v[j]); }
-            *reinterpret_cast<float4*>(z + i) = *reinterpret_cast<float4*>(v);
-        }
-    } else {
+        for (int j = 0; j < 4; ++j) v[j] = v[j] == v[j] ? v[j] : -INFINITY;
+        return make_float4(v[0], v[1], v[2], v[3]);
+    };
 #pragma unroll 8
-        for (int i = w0 + lane; i < w1; i += 32) {
-            float v = i < n_mine ? __ldcs(in + i) : -INFINITY;
-            v = v == v ? v : -INFINITY;
-            mx = fmaxf(mx, v);
-            z[i] = v;
-        }
+    for (int i = w0 + lane * 4; i < w1; i += 128) {
+        const float4 v = fetch(i);
+        mx = fmaxf(fmaxf(mx, fmaxf(v.x, v.y)), fmaxf(v.z, v.w));
+        if (kResident) *reinterpret_cast<float4*>(z + i) = v;
     }
+    auto load = [&](int i) -> float4 { return kResident ? *reinterpret_cast<const float4*>(z + i) : fetch(i); };
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -236,8 +238,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (tid < kWarps) {
         mx = __uint_as_float((uint32_t)s.warp_sum[tid][0]);
 #pragma unroll
-        for (int o = 8; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffu, mx, o));
-        if (tid < C) cluster.map_shared_rank(&s, tid)->max[rank] = mx;
+        for (int o = kWarps / 2; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync((1u << kWarps) - 1u, mx, o));
+        if (tid == 0)
+            for (int c = 0; c < C; ++c) cluster.map_shared_rank(&s, c)->max[rank] = mx;
     }
     cluster.sync();
     mx = -INFINITY;
@@ -290,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     auto warp_part = [&](auto f) -> Sums {
         Sums a = {0, 0, 0, 0};
         for (int i = w0 + lane * 4; i < w1; i += 128) {
-            const float4 v = *reinterpret_cast<const float4*>(z + i);
+            const float4 v = load(i);
             f(v.x, i, a); f(v.y, i + 1, a); f(v.z, i + 2, a); f(v.w, i + 3, a);
         }
         return {warp_sum64(a.n), warp_sum64(a.m), warp_sum64(a.o), warp_sum64(a.t)};
@@ -312,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         // outgrows its bits over a part's ids.
         const float parts = (float)(1 << p.off_bits);
         for (int i = w0 + lane * 4; i < w1; i += 128) {
-            const float4 v4 = *reinterpret_cast<const float4*>(z + i);
+            const float4 v4 = load(i);
             const float v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -329,9 +332,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             const uint32_t low = (1u << p.off_shift) - 1u;
 #pragma unroll 4
             for (int c = 0; c < C; ++c) {
-                const uint4 h = *reinterpret_cast<const uint4*>(&cluster.map_shared_rank(&s, c)->hist[tid * kPer]);
-                cnt[0] += h.x >> p.off_shift; cnt[1] += h.y >> p.off_shift; cnt[2] += h.z >> p.off_shift; cnt[3] += h.w >> p.off_shift;
-                off[0] += h.x & low; off[1] += h.y & low; off[2] += h.z & low; off[3] += h.w & low;
+#pragma unroll
+                for (int j = 0; j < kPer; j += 4) {
+                    const uint4 h = *reinterpret_cast<const uint4*>(&cluster.map_shared_rank(&s, c)->hist[tid * kPer + j]);
+                    cnt[j] += h.x >> p.off_shift; cnt[j + 1] += h.y >> p.off_shift; cnt[j + 2] += h.z >> p.off_shift; cnt[j + 3] += h.w >> p.off_shift;
+                    off[j] += h.x & low; off[j + 1] += h.y & low; off[j + 2] += h.z & low; off[j + 3] += h.w & low;
+                }
             }
             uint32_t n = 0;
             float m = 0.f, ms[kPer];
@@ -610,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                 }
                 if (rank == 0) {
                     const int n = (int)n_in;
-                    rank_list(s, n);
+                    rank_list<kThreads>(s, n);
                     if (tid == 0) s.list_at = n - 1;
                     u64 w[kPer], at;
 #pragma unroll
@@ -697,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                     const int i = i0 + lane * 4;
                     u64 w[4] = {};
                     if (i < w1) {
-                        const float4 v4 = *reinterpret_cast<const float4*>(z + i);
+                        const float4 v4 = load(i);
                         const float v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
@@ -730,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         float* const probs = p.probs ? p.probs + (size_t)row * p.V + first : nullptr;
         float* const lg = p.logits_out ? p.logits_out + (size_t)row * p.V + first : nullptr;
         for (int i = w0 + lane * 4; i < w1; i += 128) {
-            const float4 v4 = *reinterpret_cast<const float4*>(z + i);
+            const float4 v4 = load(i);
             const float v[4] = {v4.x, v4.y, v4.z, v4.w};
             float a[4], b[4];
 #pragma unroll
@@ -789,20 +795,28 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     p.vec_in = ((uintptr_t)logits & 15) == 0 && ld % 4 == 0;
     p.vec_probs = ((uintptr_t)probs & 15) == 0 && V % 4 == 0;
     p.vec_logits = ((uintptr_t)logits_out & 15) == 0 && V % 4 == 0;
-    // CTAs of a row: parts of at most 16384 ids, so that two or three CTAs share an SM; more CTAs where rows are few
+    // CTAs of a row.  Few rows (two large CTAs an SM hold them all, eight to a row): parts of at most 16384 ids in shared memory, and more
+    // CTAs where rows are fewer still.  Many: as many small CTAs to a row as four to an SM allow at once.
+    const int sms = ctx->num_sms;
+    const bool resident = (int64_t)M * 8 <= 2 * sms && V <= kMaxCluster * 16384;
+    const int threads = resident ? 512 : 256;
+    auto part = [&](int c) { return (int)(align_up((size_t)((V + c - 1) / c), (size_t)4 * threads)); };
     int C = 1;
-    auto part = [&](int c) { return (int)(align_up((size_t)((V + c - 1) / c), 4 * kThreads)); };
-    while (C < kMaxCluster && (part(C) > 16384 || (part(C) > 4 * kThreads && (int64_t)2 * C * M <= ctx->num_sms))) C <<= 1;
+    if (resident)
+        while (C < kMaxCluster && (part(C) > 16384 || (part(C) > 4 * threads && (int64_t)2 * C * M <= sms))) C <<= 1;
+    else
+        while (C < kMaxCluster && (part(C) > kMaxPart || (C < 8 && part(C) > 4 * threads && (int64_t)2 * C * M <= 4 * sms))) C <<= 1;
     p.part = part(C);
     // a histogram word: up to `part` ids counted above, their places of three bits (or one) summed below
     p.off_bits = p.part <= 16384 ? 3 : 1;
     p.off_shift = p.part <= 16384 ? 17 : 16;
-    const size_t smem = sizeof(Shared) + (size_t)p.part * sizeof(float);
-    MIRROR_CUDA_OK(cudaFuncSetAttribute(sample_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    if (C > 8) MIRROR_CUDA_OK(cudaFuncSetAttribute(sample_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    const size_t smem = sizeof(Shared) + (resident ? (size_t)p.part * sizeof(float) : 0);
+    auto kernel = resident ? sample_kernel<true, 512> : sample_kernel<false, 256>;
+    MIRROR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (C > 8) MIRROR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)C * (unsigned)M);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = (cudaStream_t)stream;
     cudaLaunchAttribute attr[2];
@@ -813,7 +827,7 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    MIRROR_CUDA_OK(cudaLaunchKernelEx(&cfg, sample_kernel, p));
+    MIRROR_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, p));
     ctx->launches += 1;
     MIRROR_CUDA_OK(cudaGetLastError());
     return MIRROR_OK;
