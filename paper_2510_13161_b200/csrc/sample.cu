@@ -37,6 +37,7 @@ constexpr int kBins = 2048;
 constexpr float kBinsPerNat = 64.f;
 constexpr int kList = 2048;                   // candidates that the leader ranks
 constexpr int kMaxCluster = 16;
+constexpr int kTable = 16;
 constexpr int kMaxPart = 40960;               // ids of a CTA
 static_assert(kBins == kList, "a thread has as many bins as candidates");
 
@@ -82,6 +83,7 @@ struct alignas(16) Shared {
     int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
     int bucket;
     float row_mass;
+    alignas(16) double table[kTable];         // 2^(j / 16)
     union alignas(16) {
         uint32_t hist[kBins];                 // counts and offsets; the leader's: then where each bin's candidates go
         Drawn drawn[kBins / 4];               // (the candidates that the draw has to look at one by one)
@@ -94,35 +96,30 @@ static_assert(sizeof(Shared) % 16 == 0, "the logits behind it are read 16 bytes 
 __device__ __forceinline__ float unkey(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ float logit_of(u64 key) { return unkey(~(uint32_t)(key >> 32)); }
 
-// round(2^S exp((l - max) / T)): y = (l - max) log2(e) / T = n + f with |f| <= 1/2, and 2^f by its Taylor series to f^11 (the next term
-// is below 7e-15).
+// round(2^S exp((l - max) / T)): y = (l - max) log2(e) / T = n / 16 + f with |f| <= 1/32; 2^(n / 16) from a table of sixteenths (16
+// doubles fill the 32 banks once, so any lanes may read any of them), 2^f by its Taylor series to f^6 (the next term is below 5e-16).
 struct Weigh {
-    double max, c;                            // c = log2(e) / T
+    double max, c;                            // c: log2(e) / T, as far as weights can tell (the next number below the maximum at 2^-900)
+    float lo, hi;                             // l is taken between them: 2^-900 is nothing, and a maximum of +inf counts as a number (c = 0)
     int shift;
-    bool max_inf;
-    __device__ __forceinline__ double exp2_scaled(double y, int s) const {      // 2^(y + s), 0 where that is below 2^-1000
-        const double magic = 6755399441055744.0;                 // 1.5 * 2^52: the sum's low bits are the nearest integer
+    const double* table;
+    __device__ __forceinline__ double y_of(float l) const { return ((double)fminf(fmaxf(l, lo), hi) - max) * c; }
+    __device__ __forceinline__ double exp2_scaled(double y, int s) const {      // 2^(y + s)
+        const double magic = 422212465065984.0;                  // 1.5 * 2^48: the sum's low bits are the nearest sixteenth
         const double t = y + magic;
         const int n = __double2loint(t);
         const double f = y - (t - magic);
-        double r = 4.4455382718708116e-10;                       // ln(2)^k / k!, k = 11 .. 0
-        r = fma(r, f, 7.0549116208011234e-09);
-        r = fma(r, f, 1.0178086009239699e-07);
-        r = fma(r, f, 1.3215486790144307e-06);
-        r = fma(r, f, 1.5252733804059840e-05);
-        r = fma(r, f, 1.5403530393381609e-04);
-        r = fma(r, f, 1.3333558146428443e-03);
-        r = fma(r, f, 9.6181291076284772e-03);
-        r = fma(r, f, 5.5504108664821580e-02);
-        r = fma(r, f, 2.4022650695910071e-01);
-        r = fma(r, f, 6.9314718055994531e-01);
+        double r = 1.54035303933816061e-04;                        // ln(2)^k / k!, k = 6 .. 0
+        r = fma(r, f, 1.33335581464284411e-03);
+        r = fma(r, f, 9.61812910762847688e-03);
+        r = fma(r, f, 5.55041086648215762e-02);
+        r = fma(r, f, 2.40226506959100694e-01);
+        r = fma(r, f, 6.93147180559945286e-01);
         r = fma(r, f, 1.0);
-        const int e = n + s;
-        if (!(y > -1000.0)) return 0.0;
-        return __hiloint2double(__double2hiint(r) + (e << 20), __double2loint(r));
+        r *= table[n & (kTable - 1)];
+        return __hiloint2double(__double2hiint(r) + (((n >> 4) + s) << 20), __double2loint(r));
     }
-    __device__ __forceinline__ double y_of(float l) const { return max_inf ? 0.0 : ((double)l - max) * c; }
-    // (of an id that may be kept: neither NaN nor -inf; where the maximum is +inf only ids of +inf may)
+    // (of an id that may be kept)
     __device__ __forceinline__ u64 operator()(float l) const {
         const double w = exp2_scaled(y_of(l), shift);
         return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;          // + 2^52: the low bits are the integer
@@ -231,6 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
     auto load = [&](int i) -> float4 { return kResident ? *reinterpret_cast<const float4*>(z + i) : fetch(i); };
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+    if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
 #pragma unroll
     for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     if (lane == 0) s.warp_sum[warp][0] = __float_as_uint(mx);
@@ -258,19 +256,25 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     const double min_p = p.min_p && !first_only ? (double)p.min_p[row] : 0.0;
     const bool by_m = min_p > 0.0;
     const bool whole_total = by_p && !by_k;                      // Top-p of the whole row
+    const bool max_inf = mx == INFINITY, none = mx == -INFINITY; // (none: nothing to keep)
     Weigh weigh;
-    weigh.max = (double)mx;
-    weigh.c = 1.4426950408889634074 / (double)T;
+    weigh.hi = fminf(fmaxf(mx, -3.4028235e38f), 3.4028235e38f);
+    weigh.max = (double)weigh.hi;
+    const double c = max_inf || none ? 0.0 : 1.4426950408889634074 / (double)T;
+    const float below = nextafterf(weigh.hi, -INFINITY);
+    weigh.c = fmin(c, below > -INFINITY ? 900.0 / (weigh.max - (double)below) : 1e300);
+    weigh.lo = fmaxf(fminf((float)fmax(weigh.max - 900.0 / weigh.c, -3.4e38), below), -3.4028235e38f);
     weigh.shift = p.shift;
-    weigh.max_inf = mx == INFINITY;
-    auto may = [&](float l) { return weigh.max_inf ? l == INFINITY : l > -INFINITY; };
-    const bool none = mx == -INFINITY;                           // (nothing to keep)
+    weigh.table = s.table;
+    // ids that may be kept: neither NaN nor -inf, and where the maximum is +inf only those
+    const float least = max_inf ? INFINITY : -3.4028235e38f;
+    auto may = [&](float l) { return l >= least; };
     const u64 min_w = by_m ? (u64)fmin(ceil(min_p * exp2((double)p.shift)), exp2((double)p.shift)) : 0ull;
     // composite key of an id: smaller is ahead
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
     const float inv_T = 1.f / T;
     auto bin_of = [&](float l, float& at) {
-        at = weigh.max_inf ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));
+        at = max_inf ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));
         return (int)at;
     };
     int turn = 0;
@@ -667,7 +671,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         }
     }
     // ---- 5: the warps' kept masses, the draw, the distribution
-    auto kept = [&](float l, int i) { return may(l) && key_of(l, first + i) <= cut; };
+    const float cut_l = cut == ~0ull ? least : fmaxf(logit_of(cut), least);
+    const int cut_i = cut == ~0ull ? 0x7fffffff : (int)min((uint32_t)cut, 0x7fffffffu) - first;
+    auto kept = [&](float l, int i) { return l > cut_l || (l == cut_l && i <= cut_i); };
     if (!listed) {
         // (ahead of the bin in which the front ends the masses are known)
         const Sums mine = warp_part([&](float l, int i, Sums& a) {
@@ -743,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             for (int j = 0; j < 4; ++j) {
                 const bool in_front = kept(v[j], i + j);
                 a[j] = in_front && probs ? (float)(weigh.exact(v[j]) * inv) : 0.f;
-                b[j] = in_front && lg ? (float)(weigh.y_of(v[j]) * ln2T - ln_z * (double)p.temperature) : -INFINITY;
+                b[j] = in_front && lg ? (float)((max_inf ? 0.0 : ((double)v[j] - weigh.max) * c) * ln2T - ln_z * (double)p.temperature) : -INFINITY;
             }
             const bool whole = i + 4 <= n_mine;
             if (probs) {
