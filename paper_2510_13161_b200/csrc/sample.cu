@@ -11,11 +11,12 @@
 // the time then is the steps that one CTA, or one thread, takes for its row while the others wait, so four small CTAs an SM, each with
 // more of a row, get more rows through than two large ones (520 rows: 541 -> MEASURED us).
 //   1  load, maximum over the cluster (the logits leave HBM once)
-//   2  a histogram of z in 2048 bins of 1/64: how many ids each holds and where in the bin they lie on average, packed in one word, which
-//      gives a bin's mass to 10^-3
+//   2  Top-k of up to kQuickK: a histogram of the largest of every four logits says down to which logit at least k ids lie; Min-p says
+//      so by itself.  Top-p of the whole row: a histogram of z in 2048 bins of 1/64, how many ids each holds and where in the bin they lie on
+//      average, packed in one word, which gives a bin's mass to 10^-3
 //   3  the leading CTA adds the histograms up and reads off the bin in which each filter's front ends, Top-p's by estimate
-//   4  if at most kList ids lie ahead of a bin that surely lies behind the end of the front, they go to the leader, in the order of their bins;
-//      it ranks those of a bin among themselves and does the rest.  Top-p's exact total is taken in the same pass
+//   4  if at most kList ids lie ahead of a logit that surely lies behind the end of the front, they go to the leader, which ranks them and
+//      does the rest, while the others fill the distribution's rows.  Top-p's exact total is taken in the same pass
 //   4' otherwise only the bin in which the front ends goes to the leader; what lies ahead of it is counted and summed by all.  (A bin
 //      of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
 //   5  the drawn token, by the warps' masses, and the filtered distribution
@@ -38,6 +39,7 @@ constexpr float kBinsPerNat = 64.f;
 constexpr int kList = 2048;                   // candidates that the leader ranks
 constexpr int kMaxCluster = 16;
 constexpr int kTable = 16;
+constexpr int kQuickK = 1400;                 // (the largest of every four: hardly more than k candidates then)
 constexpr int kMaxPart = 40960;               // ids of a CTA
 static_assert(kBins == kList, "a thread has as many bins as candidates");
 
@@ -79,7 +81,8 @@ struct alignas(16) Shared {
     u64 cut_key;                              // composite key of the last kept id
     u64 kept;                                 // its front's mass
     u64 base;
-    int last_bin, n_list, list_at;            // written by the leader
+    int last_bin, list_at;                    // written by the leader
+    int n_list;
     int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
     int bucket;
     float row_mass;
@@ -142,35 +145,6 @@ __device__ __forceinline__ u64 warp_incl64(u64 v) {
     return v;
 }
 
-// list[0 .. n) ranked, by comparing all with all.
-template <int kThreads>
-__device__ __noinline__ void rank_list(Shared& s, int n) {
-    constexpr int kPer = kList / kThreads;
-    const int tid = threadIdx.x;
-    __syncthreads();
-    u64 key[kPer];
-    int at[kPer];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        key[j] = tid + j * kThreads < n ? s.list[tid + j * kThreads] : ~0ull;
-        at[j] = 0;
-    }
-    const int rounds = (n + kThreads - 1) / kThreads;            // (elements of a thread that there are)
-#pragma unroll 4
-    for (int q = 0; q < n; ++q) {
-        const u64 k = s.list[q];
-        at[0] += k < key[0];
-        if (rounds > 1) {
-#pragma unroll
-            for (int j = 1; j < kPer; ++j) at[j] += k < key[j];
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-        if (tid + j * kThreads < n) s.ranked[at[j]] = key[j];
-    __syncthreads();
-}
-
 // A thread's w[], inclusive over the block: what lies before it, and all.
 template <int kPer>
 __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& before) {
@@ -187,6 +161,50 @@ __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& 
     all = warp_incl64(all);
     before = in - mine + (warp ? __shfl_sync(0xffffffffu, all, warp - 1) : 0ull);
     return __shfl_sync(0xffffffffu, all, kWarps - 1);
+}
+
+// list[0 .. n) in ascending order: sorted into bins over the logits from `hi` down, `scale` of them to a nat of it, and within a bin by
+// comparing all with all.
+template <int kThreads>
+__device__ __noinline__ void sort_list(Shared& s, int n, float hi, float scale) {
+    constexpr int kPer = kList / kThreads;
+    const int tid = threadIdx.x;
+    auto place = [&](u64 key) { return (int)fminf(fmaxf((hi - logit_of(key)) * scale, 0.f), (float)(kBins - 1)); };
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+    __syncthreads();
+    u64 key[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        key[j] = tid + j * kThreads < n ? s.list[tid + j * kThreads] : ~0ull;
+        if (tid + j * kThreads < n) atomicAdd(&s.hist[place(key[j])], 1u);
+    }
+    __syncthreads();
+    {
+        u64 cnt[kPer], before;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) cnt[j] = s.hist[tid * kPer + j];
+        block_scan(s, cnt, before);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            s.hist[tid * kPer + j] = (uint32_t)before;
+            before += cnt[j];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (tid + j * kThreads < n) s.ranked[atomicAdd(&s.hist[place(key[j])], 1u)] = key[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (tid + j * kThreads >= n) break;
+        const int b = place(key[j]), lo = b ? (int)s.hist[b - 1] : 0, end = (int)s.hist[b];
+        int ahead = 0;
+        for (int q = lo; q < end; ++q) ahead += s.ranked[q] < key[j];
+        s.list[lo + ahead] = key[j];
+    }
+    __syncthreads();
 }
 
 template <bool kResident, int kThreads>
@@ -266,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     weigh.lo = fmaxf(fminf((float)fmax(weigh.max - 900.0 / weigh.c, -3.4e38), below), -3.4028235e38f);
     weigh.shift = p.shift;
     weigh.table = s.table;
+    const double ln2T = 0.69314718055994530942 * (double)p.temperature;
     // ids that may be kept: neither NaN nor -inf, and where the maximum is +inf only those
     const float least = max_inf ? INFINITY : -3.4028235e38f;
     auto may = [&](float l) { return l >= least; };
@@ -311,165 +330,216 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     };
 
     u64 cut = ~0ull;                                             // composite key of the last id of the front
-    bool listed = false;
-    int ahead_bin = -1;                                          // >= 0: the warps' masses ahead of that bin are in s.warp_mass, with their counts
+    int ahead_bin = -1;                                          // >= 0: the warps' masses ahead of that bin are in s.warp_mass
     u64 Z = 0;
     if (!none && (by_k || by_p || by_m)) {
-        // ---- 2: histogram.  A word counts in its upper bits and sums in its lower ones in which part of the bin the ids lie: neither half
-        // outgrows its bits over a part's ids.
         const float parts = (float)(1 << p.off_bits);
-        for (int i = w0 + lane * 4; i < w1; i += 128) {
-            const float4 v4 = load(i);
-            const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (!may(v[j])) continue;
-                float at;
-                const int bin = bin_of(v[j], at);
-                atomicAdd(&s.hist[bin], (1u << p.off_shift) + (uint32_t)((at - (float)bin) * parts));
-            }
-        }
-        cluster.sync();
-        // ---- 3: the bins in which the fronts end
-        if (rank == 0) {
-            uint32_t cnt[kPer] = {}, off[kPer] = {};
-            const uint32_t low = (1u << p.off_shift) - 1u;
-#pragma unroll 4
-            for (int c = 0; c < C; ++c) {
-#pragma unroll
-                for (int j = 0; j < kPer; j += 4) {
-                    const uint4 h = *reinterpret_cast<const uint4*>(&cluster.map_shared_rank(&s, c)->hist[tid * kPer + j]);
-                    cnt[j] += h.x >> p.off_shift; cnt[j + 1] += h.y >> p.off_shift; cnt[j + 2] += h.z >> p.off_shift; cnt[j + 3] += h.w >> p.off_shift;
-                    off[j] += h.x & low; off[j + 1] += h.y & low; off[j + 2] += h.z & low; off[j + 3] += h.w & low;
-                }
-            }
-            uint32_t n = 0;
-            float m = 0.f, ms[kPer];
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                // (the mean of exp(-x) over a 64th is exp(-mean) but for a relative 10^-4; the last bin is open: no mass)
-                const int b = tid * kPer + j;
-                const float mean = ((float)b + __fdividef((float)off[j] + 0.5f * (float)cnt[j], parts * fmaxf((float)cnt[j], 1.f))) * (1.f / kBinsPerNat);
-                ms[j] = b == kBins - 1 ? 0.f : (float)cnt[j] * __expf(-mean);
-                n += cnt[j];
-                m += ms[j];
-            }
-            // exclusive sums over the threads
-            uint32_t n_in = n;
-            float m_in = m;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t a = __shfl_up_sync(0xffffffffu, n_in, o);
-                const float b = __shfl_up_sync(0xffffffffu, m_in, o);
-                if (lane >= o) { n_in += a; m_in += b; }
-            }
-            if (lane == 31) s.warp_sum[warp][0] = ((u64)n_in << 32) | __float_as_uint(m_in);
-            if (tid == 0) {
-                s.last_bin = s.bin_k = s.bin_p = kBins - 1;
-                s.list_at = 0;
-            }
-            __syncthreads();
-            float m_all = 0.f;
-            uint32_t n_before = n_in - n;
-            float m_before = m_in - m;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const u64 t = s.warp_sum[w][0];
-                if (w < warp) { n_before += (uint32_t)(t >> 32); m_before += __uint_as_float((uint32_t)t); }
-                m_all += __uint_as_float((uint32_t)t);
-            }
-            if (tid == 0) s.row_mass = m_all;
-            __syncthreads();
-            // Top-k's bin, and about what its front weighs
-            if (by_k) {
-                uint32_t nb = n_before;
-                float mb = m_before;
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    if (nb < (uint32_t)k && nb + cnt[j] >= (uint32_t)k) {
-                        s.bin_k = tid * kPer + j;
-                        s.row_mass = mb + ms[j] * (float)((uint32_t)k - nb) / (float)cnt[j];
-                    }
-                    nb += cnt[j];
-                    mb += ms[j];
-                }
-                __syncthreads();
-            }
-            // (Top-p behind Top-k is a share of all that Top-k leaves: then nothing else shortens the list)
-            const float about = (float)top_p * s.row_mass, m_at = -logf((float)fmin(min_p, 1.0)) * kBinsPerNat + 1.f;
-            const bool p_ends = whole_total, m_ends = by_m && !(by_k && by_p);
-            uint32_t nb = n_before;
-            float mb = m_before;
-            int end = kBins - 1, end_p = kBins - 1;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const int b = tid * kPer + j;
-                nb += cnt[j];
-                mb += ms[j];
-                // the first bin at which one of the filters is surely through
-                if ((by_k && nb >= (uint32_t)k) || (p_ends && mb >= 1.01f * about) || (m_ends && (float)b >= m_at)) end = min(end, b);
-                if (by_p && mb >= about) end_p = min(end_p, b);
-            }
-            end = __reduce_min_sync(0xffffffffu, end);
-            end_p = __reduce_min_sync(0xffffffffu, end_p);
-            if (lane == 0) {
-                atomicMin(&s.last_bin, end);
-                atomicMin(&s.bin_p, end_p);
-            }
-            __syncthreads();
-            // how many ids that is, and where each bin's go
-            nb = n_before;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                s.hist[tid * kPer + j] = nb;
-                nb += cnt[j];
-                if (tid * kPer + j == s.last_bin) s.n_list = (int)nb;
-            }
-            __syncthreads();
-            if (tid < C) {
-                Shared* const o = cluster.map_shared_rank(&s, tid);
-                o->last_bin = s.last_bin;
-                o->bin_k = s.bin_k;
-                o->bin_p = s.bin_p;
-                o->n_list = s.n_list;
-            }
-        }
-        cluster.sync();
-        const int n_list = s.n_list, last_bin = s.last_bin;
-        listed = n_list <= kList;
-        if (listed) {
-            // ---- 4: the leader's list, and Top-p's total
-            const Sums a = warp_part([&](float l, int i, Sums& a) {
-                if (!may(l)) return;
-                if (whole_total) a.m += weigh(l);
-                float at;
-                const int bin = bin_of(l, at);
-                if (bin > last_bin) return;
-                const uint32_t slot = atomicAdd(&lead->hist[bin], 1u);
-                if (slot < (uint32_t)kList) lead->list[slot] = key_of(l, first + i);
-            });
-            __syncthreads();
-            if (lane == 0) { s.warp_sum[warp][0] = s.warp_sum[warp][2] = s.warp_sum[warp][3] = 0; s.warp_sum[warp][1] = a.m; }
-            const u64 total = exchange().m;
+        // ---- 3: the leader's reading of the histograms.  `masses`: the words hold offsets, too.
+        auto read_bins = [&](bool masses) {
+            cluster.sync();
             if (rank == 0) {
-                // ranks: the bin's place, and the place within the bin
+                uint32_t cnt[kPer] = {}, off[kPer] = {};
+                const uint32_t low = (1u << p.off_shift) - 1u;
+#pragma unroll 4
+                for (int c = 0; c < C; ++c) {
+#pragma unroll
+                    for (int j = 0; j < kPer; j += 4) {
+                        const uint4 h = *reinterpret_cast<const uint4*>(&cluster.map_shared_rank(&s, c)->hist[tid * kPer + j]);
+                        cnt[j] += h.x >> p.off_shift; cnt[j + 1] += h.y >> p.off_shift; cnt[j + 2] += h.z >> p.off_shift; cnt[j + 3] += h.w >> p.off_shift;
+                        off[j] += h.x & low; off[j + 1] += h.y & low; off[j + 2] += h.z & low; off[j + 3] += h.w & low;
+                    }
+                }
+                uint32_t n = 0;
+                float m = 0.f, ms[kPer];
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
-                    const int r = tid + j * kThreads;
-                    if (r >= n_list) break;
-                    const u64 key = s.list[r];
-                    float at;
-                    const int bin = bin_of(logit_of(key), at), lo = bin ? (int)s.hist[bin - 1] : 0, hi = (int)s.hist[bin];
-                    int ahead = 0;
-                    for (int q = lo; q < hi; ++q) ahead += s.list[q] < key;
-                    s.ranked[lo + ahead] = key;
+                    // (the mean of exp(-x) over a 64th is exp(-mean) but for a relative 10^-4; the last bin is open: no mass)
+                    const int b = tid * kPer + j;
+                    const float mean = ((float)b + __fdividef((float)off[j] + 0.5f * (float)cnt[j], parts * fmaxf((float)cnt[j], 1.f))) * (1.f / kBinsPerNat);
+                    ms[j] = b == kBins - 1 ? 0.f : (float)cnt[j] * __expf(-mean);
+                    n += cnt[j];
+                    m += ms[j];
                 }
+                // exclusive sums over the threads
+                uint32_t n_in = n;
+                float m_in = m;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint32_t a = __shfl_up_sync(0xffffffffu, n_in, o);
+                    const float b = __shfl_up_sync(0xffffffffu, m_in, o);
+                    if (lane >= o) { n_in += a; m_in += b; }
+                }
+                if (lane == 31) s.warp_sum[warp][0] = ((u64)n_in << 32) | __float_as_uint(m_in);
+                if (tid == 0) s.last_bin = s.bin_k = s.bin_p = kBins - 1;
                 __syncthreads();
+                float m_all = 0.f;
+                uint32_t n_before = n_in - n;
+                float m_before = m_in - m;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const u64 t = s.warp_sum[w][0];
+                    if (w < warp) { n_before += (uint32_t)(t >> 32); m_before += __uint_as_float((uint32_t)t); }
+                    m_all += __uint_as_float((uint32_t)t);
+                }
+                if (tid == 0) s.row_mass = m_all;
+                __syncthreads();
+                // Top-k's bin, and about what its front weighs
+                if (by_k) {
+                    uint32_t nb = n_before;
+                    float mb = m_before;
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        if (nb < (uint32_t)k && nb + cnt[j] >= (uint32_t)k) {
+                            s.bin_k = tid * kPer + j;
+                            s.row_mass = mb + ms[j] * (float)((uint32_t)k - nb) / (float)cnt[j];
+                        }
+                        nb += cnt[j];
+                        mb += ms[j];
+                    }
+                    __syncthreads();
+                }
+                if (masses && by_p) {
+                    const float about = (float)top_p * s.row_mass;
+                    float mb = m_before;
+                    int end = kBins - 1, end_p = kBins - 1;
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        const int b = tid * kPer + j;
+                        mb += ms[j];
+                        // the first bin at which Top-p is surely through, and where it ends by estimate
+                        if (mb >= 1.01f * about) end = min(end, b);
+                        if (mb >= about) end_p = min(end_p, b);
+                    }
+                    end = __reduce_min_sync(0xffffffffu, end);
+                    end_p = __reduce_min_sync(0xffffffffu, end_p);
+                    if (lane == 0) {
+                        atomicMin(&s.last_bin, end);
+                        atomicMin(&s.bin_p, end_p);
+                    }
+                    __syncthreads();
+                }
+                // how many ids that is
+                uint32_t nb = n_before;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    nb += cnt[j];
+                    if (tid * kPer + j == s.last_bin) s.n_list = (int)nb;
+                }
+                // (Top-p behind Top-k is a share of all that Top-k leaves, so Top-k's end counts alone)
+                if (tid == 0 && by_k) s.last_bin = s.bin_k;
+                __syncthreads();
+                if (tid < C) {
+                    Shared* const o = cluster.map_shared_rank(&s, tid);
+                    o->last_bin = s.last_bin;
+                    o->bin_k = s.bin_k;
+                    o->bin_p = s.bin_p;
+                    o->n_list = s.n_list;
+                }
+            }
+            cluster.sync();
+        };
+        // a logit below all of the bins up to b, and one that Min-p surely leaves out
+        const float slack = fabsf(weigh.hi) * 1e-6f;
+        auto below_bin = [&](int b) { return b >= kBins - 1 || max_inf ? least : weigh.hi - (float)(b + 1) * T * (1.00002f / kBinsPerNat) - slack; };
+        const float below_m = by_m && !max_inf ? weigh.hi + T * (logf((float)fmin(min_p, 1.0)) * 1.00002f - 1e-5f) - slack : least;
+        // ---- 4: the ids from `from` on to the leader, and (of_all) the mass of all.  How many they are:
+        u64 total = 0;
+        auto push = [&](float from, bool of_all) -> int {
+            if (rank == 0 && tid == 0) s.list_at = 0;
+            cluster.sync();
+            Sums a = {0, 0, 0, 0};
+            for (int i = w0 + lane * 4; i < w1; i += 128) {
+                const float4 v4 = load(i);
+                const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+                if (of_all) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (may(v[j])) a.m += weigh(v[j]);
+                }
+                if (fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= from) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (v[j] >= from) {
+                            ++a.n;
+                            const int slot = atomicAdd(&lead->list_at, 1);
+                            if (slot < kList) lead->list[slot] = key_of(v[j], first + i + j);
+                        }
+                }
+            }
+            a.n = warp_sum64(a.n);
+            a.m = warp_sum64(a.m);
+            __syncthreads();
+            if (lane == 0) { s.warp_sum[warp][0] = a.n; s.warp_sum[warp][1] = a.m; s.warp_sum[warp][2] = s.warp_sum[warp][3] = 0; }
+            a = exchange();
+            total = a.m;
+            return a.n > (u64)kList ? kList + 1 : (int)a.n;
+        };
+        float from = least;
+        int n_list = kList + 1;
+        const bool quick = by_k ? k <= kQuickK : by_m && !by_p;
+        // ---- 2: histograms.  A word counts in its upper bits and sums in its lower ones in which part of the bin the ids lie: neither half
+        // outgrows its bits over a part's ids.
+        if (quick) {
+            if (by_k) {
+                for (int i = w0 + lane * 4; i < w1; i += 128) {
+                    const float4 v = load(i);
+                    const float top = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
+                    float at;
+                    if (may(top)) atomicAdd(&s.hist[bin_of(top, at)], 1u << p.off_shift);
+                }
+                read_bins(false);
+                from = below_bin(s.last_bin);
+            }
+            if (!(by_k && by_p)) from = fmaxf(from, below_m);
+            from = from >= least ? from : least;
+            n_list = push(from, false);
+        }
+        if (n_list > kList) {
+            __syncthreads();
+            for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
+            __syncthreads();
+            for (int i = w0 + lane * 4; i < w1; i += 128) {
+                const float4 v4 = load(i);
+                const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!may(v[j])) continue;
+                    float at;
+                    const int bin = bin_of(v[j], at);
+                    atomicAdd(&s.hist[bin], (1u << p.off_shift) + (uint32_t)((at - (float)bin) * parts));
+                }
+            }
+            read_bins(true);
+            if (!by_k && by_p && (by_m || s.n_list <= kList)) {  // (the others have been tried, or have no list that is short enough)
+                from = fmaxf(below_bin(s.last_bin), below_m);
+                from = from >= least ? from : least;
+                n_list = push(from, whole_total);
+            }
+        }
+        if (n_list <= kList) {
+            // the distribution's rows: the others fill them while the leader ranks (nobody reads the logits any more)
+            if (rank != 0 || C == 1) {
+                auto fill = [&](float* out, float what, bool vec) {
+                    const int workers = C == 1 ? 1 : C - 1, me = C == 1 ? 0 : rank - 1;
+                    if (vec) {
+                        float4* const o = reinterpret_cast<float4*>(out);
+                        for (int i = me * kThreads + tid; i < p.V / 4; i += workers * kThreads) __stcs(o + i, make_float4(what, what, what, what));
+                    } else {
+                        for (int i = me * kThreads + tid; i < p.V; i += workers * kThreads) out[i] = what;
+                    }
+                };
+                if (p.probs) fill(p.probs + (size_t)row * p.V, 0.f, p.vec_probs);
+                if (p.logits_out) fill(p.logits_out + (size_t)row * p.V, -INFINITY, p.vec_logits);
+            }
+            if (rank == 0) {
+                sort_list<kThreads>(s, n_list, weigh.hi, weigh.hi - from > 0.f && !max_inf ? (float)(kBins - 1) / (weigh.hi - from) : 0.f);
+                u64 key[kPer];
                 u64 w[kPer], sel[kPer], before;
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
                     const int r = tid * kPer + j;
-                    w[j] = r < n_list ? weigh(logit_of(s.ranked[r])) : 0ull;
+                    key[j] = r < n_list ? s.list[r] : ~0ull;
+                    w[j] = r < n_list ? weigh(logit_of(key[j])) : 0ull;
                     sel[j] = by_k && r >= k ? 0ull : w[j];
                 }
                 const u64 part = block_scan(s, sel, before);
@@ -488,26 +558,21 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 kept_mass = warp_sum64(kept_mass);
                 if (lane == 0) { s.warp_sum[warp][2] = (u64)kept; s.warp_sum[warp][3] = kept_mass; }
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) s.list[tid * kPer + j] = 0;           // (from here on: masses of buckets of ids)
+                for (int j = 0; j < kPer; ++j) s.ranked[tid * kPer + j] = 0;         // (from here on: masses of buckets of ids)
                 if (tid == 0) s.list_at = 0;
                 __syncthreads();
                 int n = 0;
                 Z = 0;
 #pragma unroll
                 for (int q = 0; q < kWarps; ++q) { n += (int)s.warp_sum[q][2]; Z += s.warp_sum[q][3]; }
-                if (tid < C && (p.probs || p.logits_out)) {
-                    Shared* const o = cluster.map_shared_rank(&s, tid);
-                    o->cut_key = s.ranked[n - 1];
-                    o->kept = Z;
-                }
                 // the draw: the bucket of ids in which the sum over ids passes the uniform's share, then the id within it
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
-                    if (tid * kPer + j < n) atomicAdd(&s.list[(uint32_t)s.ranked[tid * kPer + j] >> p.id_shift], w[j]);
+                    if (tid * kPer + j < n) atomicAdd(&s.ranked[(uint32_t)key[j] >> p.id_shift], w[j]);
                 __syncthreads();
                 u64 bucket[kPer];
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) bucket[j] = s.list[tid * kPer + j];
+                for (int j = 0; j < kPer; ++j) bucket[j] = s.ranked[tid * kPer + j];
                 block_scan(s, bucket, before);
                 const double t = fmax((double)p.u[row], 0.0) * (double)Z;
                 const u64 target = t >= (double)Z ? Z - 1 : (u64)t;                 // the first id whose inclusive sum is above it
@@ -521,10 +586,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 }
                 __syncthreads();
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const uint32_t id = (uint32_t)s.ranked[tid * kPer + j];
-                    if (tid * kPer + j < n && (int)(id >> p.id_shift) == s.bucket) s.drawn[atomicAdd(&s.list_at, 1)] = {w[j], id, 0u};
-                }
+                for (int j = 0; j < kPer; ++j)
+                    if (tid * kPer + j < n && (int)((uint32_t)key[j] >> p.id_shift) == s.bucket) s.drawn[atomicAdd(&s.list_at, 1)] = {w[j], (uint32_t)key[j], 0u};
                 __syncthreads();
                 for (int q = tid; q < s.list_at; q += kThreads) {
                     const Drawn d = s.drawn[q];
@@ -537,12 +600,23 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         if (p.n_kept) p.n_kept[row] = n;
                     }
                 }
+                if (!p.probs && !p.logits_out) return;
+                cluster.sync();                                  // (the rows are filled)
+                const double unit = (double)Z * exp2(-(double)p.shift), inv = 1.0 / unit, ln_z = log(unit);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    if (tid * kPer + j >= n) break;
+                    const float l = logit_of(key[j]);
+                    const size_t at = (size_t)row * p.V + (uint32_t)key[j];
+                    if (p.probs) p.probs[at] = (float)(weigh.exact(l) * inv);
+                    if (p.logits_out) p.logits_out[at] = (float)((max_inf ? 0.0 : ((double)l - weigh.max) * c) * ln2T - ln_z * (double)p.temperature);
+                }
+                return;
             }
-            if (!p.probs && !p.logits_out) return;
-            cluster.sync();
-            cut = s.cut_key;
-            Z = s.kept;
-        } else {
+            if (p.probs || p.logits_out) cluster.sync();
+            return;
+        }
+        {
             // ---- 4': the bin in which each filter's front ends, and where in it
             auto front = [&](u64 at) {                           // (count, mass) of the ids up to the composite key `at`
                 return all_sums([&](float l, int i, Sums& a) {
@@ -620,13 +694,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 }
                 if (rank == 0) {
                     const int n = (int)n_in;
-                    rank_list<kThreads>(s, n);
+                    // (the bin's range; the last bin is open, and goes by comparing)
+                    sort_list<kThreads>(s, n, weigh.hi - (float)b * T * (1.f / kBinsPerNat), max_inf || b == kBins - 1 ? 0.f : (float)(kBins - 1) * kBinsPerNat * inv_T);
                     if (tid == 0) s.list_at = n - 1;
                     u64 w[kPer], at;
 #pragma unroll
                     for (int j = 0; j < kPer; ++j) {
                         const int r = tid * kPer + j;
-                        w[j] = by_mass && r < n ? weigh(logit_of(s.ranked[r])) : 0ull;
+                        w[j] = by_mass && r < n ? weigh(logit_of(s.list[r])) : 0ull;
                     }
                     block_scan(s, w, at);
                     at += m0;
@@ -637,14 +712,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         if (r < n && done(n0 + r + 1, at, all)) { atomicMin(&s.list_at, r); break; }
                     }
                     __syncthreads();
-                    if (tid < C) cluster.map_shared_rank(&s, tid)->cut_key = s.ranked[s.list_at];
+                    if (tid < C) cluster.map_shared_rank(&s, tid)->cut_key = s.list[s.list_at];
                 }
                 cluster.sync();
                 const u64 c = s.cut_key;
                 cluster.sync();                                  // (the next one may be written)
                 return c;
             };
-            u64 total = 0;
+            total = 0;
             if (by_k) {
                 cut = end_of(s.bin_k, false, false, [&](u64 n, u64, u64) { return n >= (u64)k; });
                 if (by_p) total = front(cut).m;
@@ -674,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     const float cut_l = cut == ~0ull ? least : fmaxf(logit_of(cut), least);
     const int cut_i = cut == ~0ull ? 0x7fffffff : (int)min((uint32_t)cut, 0x7fffffffu) - first;
     auto kept = [&](float l, int i) { return l > cut_l || (l == cut_l && i <= cut_i); };
-    if (!listed) {
+    {
         // (ahead of the bin in which the front ends the masses are known)
         const Sums mine = warp_part([&](float l, int i, Sums& a) {
             if (!kept(l, i)) return;
@@ -738,7 +813,6 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
     if (p.probs || p.logits_out) {
         const double unit = (double)Z * exp2(-(double)p.shift), inv = 1.0 / unit, ln_z = log(unit);
-        const double ln2T = 0.69314718055994530942 * (double)p.temperature;
         float* const probs = p.probs ? p.probs + (size_t)row * p.V + first : nullptr;
         float* const lg = p.logits_out ? p.logits_out + (size_t)row * p.V + first : nullptr;
         for (int i = w0 + lane * 4; i < w1; i += 128) {
