@@ -237,6 +237,7 @@ class Mirror:
         self.device = torch.device("cuda", device)
         self._ctx = C.c_void_p()
         _check(self.lib.mirror_create(C.byref(self._ctx), C.byref(self.desc), device), "mirror_create")
+        self._heads = (n_q_heads, n_kv_heads, head_dim)
         self._ws = None
         self._need = {}              # workspace bytes by (what, batch, nodes): they depend on nothing else
         self._keep = []
@@ -469,51 +470,52 @@ class Mirror:
                                          factor, original_len, low, high, amplitude), "mirror_rope_init")
         return out
 
-    def _strided(self, t: torch.Tensor, heads: int, rows: Rows, name: str):
+    def _strided(self, t: torch.Tensor, shape: tuple, name: str):
         """Address, row and layer stride of a bf16 tensor [L, R, heads, d] whose heads and elements are contiguous."""
-        d = self.desc.head_dim
         if not t.is_cuda or t.dtype is not torch.bfloat16:
             raise ValueError(f"{name} must be a CUDA tensor of torch.bfloat16")
-        if t.dim() != 4 or t.shape[1] != rows.n_rows or t.shape[2] != heads or t.shape[3] != d:
-            raise ValueError(f"{name} must be [L, {rows.n_rows}, {heads}, {d}], got {tuple(t.shape)}")
-        st = t.stride()
-        if st[3] != 1 or (heads > 1 and st[2] != d):
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+        layer, row, head, one = t.stride()
+        L, R, heads, d = shape
+        if one != 1 or (head != d and heads > 1):
             raise ValueError(f"{name}: heads and elements must be contiguous")
-        # (a stride of a dimension of one entry may be anything)
-        row = st[1] if t.shape[1] > 1 else heads * d
-        return t.data_ptr(), row, st[0] if t.shape[0] > 1 else row * t.shape[1]
+        if R <= 1:                           # (a stride of a dimension of one entry may be anything)
+            row = heads * d
+        return t.data_ptr(), row, layer if L > 1 else row * R
 
     def mirror_kv_append(self, kv: KV, rows: Rows, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
                          rope: Optional[Rope] = None, q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
         """k, v [L, R, Hkv, d] into the cache's pages (keys turned to their positions), q [L, R, Hq, d] turned into q_out; the three may
         be columns of one tensor.  Returns q_out."""
-        Hq, Hkv, d = self.desc.n_q_heads, self.desc.n_kv_heads, self.desc.head_dim
-        kp, kv_row, kv_layer = self._strided(k, Hkv, rows, "k")
-        vp, v_row, v_layer = self._strided(v, Hkv, rows, "v")
-        if (v_row, v_layer) != (kv_row, kv_layer):
+        Hq, Hkv, d = self._heads
+        L, R = kv.num_layers, rows.n_rows
+        shape = (L, R, Hkv, d)
+        kp, kv_row, kv_layer = self._strided(k, shape, "k")
+        vp, v_row, v_layer = self._strided(v, shape, "v")
+        if v_row != kv_row or v_layer != kv_layer:
             raise ValueError("k and v must have the same strides")
-        if k.shape[0] != kv.num_layers or v.shape[0] != kv.num_layers:
-            raise ValueError("k and v must have the cache's layers")
-        qp, q_row, q_layer = None, 0, 0
+        qp, q_row, q_layer, op = None, 0, 0, None
         if q is not None:
-            qp, q_row, q_layer = self._strided(q, Hq, rows, "q")
+            shape = (L, R, Hq, d)
+            qp, q_row, q_layer = self._strided(q, shape, "q")
             if q_out is None:
-                q_out = torch.empty((kv.num_layers, rows.n_rows, Hq, d), dtype=torch.bfloat16, device=self.device)
-            if q.shape[0] != kv.num_layers or q_out.shape != q.shape:
-                raise ValueError("q and q_out must be [L, R, Hq, d] with the cache's layers")
+                q_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            elif q_out.shape != shape:
+                raise ValueError(f"q_out must be {shape}, got {tuple(q_out.shape)}")
+            op = _ptr(q_out, torch.bfloat16, "q_out")
         _check(self.lib.mirror_kv_append(self._ctx, C.byref(kv), C.byref(rows), C.byref(rope) if rope is not None else None, qp, q_row, q_layer,
-                                         _ptr(q_out, torch.bfloat16, "q_out") if q is not None else None, kp, vp, kv_row, kv_layer,
-                                         _stream(stream)), "mirror_kv_append")
+                                         op, kp, vp, kv_row, kv_layer, _stream(stream)), "mirror_kv_append")
         return q_out
 
     def mirror_attn_causal(self, kv: KV, rows: Rows, q: torch.Tensor, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
                            lse_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Causal attention of the rows [L, R, Hq, d] over the cache (their own keys and values appended before); window tokens and the
         first `sinks` are visible (window 0: all).  lse_out: fp32 [L, R, Hq]."""
-        shape = (kv.num_layers, rows.n_rows, self.desc.n_q_heads, self.desc.head_dim)
+        shape = (kv.num_layers, rows.n_rows, self._heads[0], self._heads[2])
         if out is None:
             out = torch.empty_like(q)
-        if tuple(q.shape) != shape or tuple(out.shape) != shape or (lse_out is not None and tuple(lse_out.shape) != shape[:3]):
+        if q.shape != shape or out.shape != shape or (lse_out is not None and lse_out.shape != shape[:3]):
             raise ValueError(f"q and out must be {shape}, lse_out {shape[:3]}")
         key = ("rows", rows.batch, rows.n_rows)
         need = self._need.get(key)

@@ -51,19 +51,20 @@ struct Request {
     int sink_slots, from, slots;
     __device__ __forceinline__ int slot_page(int t) const { return t < sink_slots ? t : t - sink_slots + from; }
 };
-// Row start, rows and prefix as they are usable: within the tensors and the page table whatever the device arrays hold.
+// Row start, rows and prefix as they are usable: within the tensors and the page table whatever the device arrays hold.  (Past L1, which
+// may hold what a look ahead of the kernel in front has seen.)
 __device__ __forceinline__ void load_request(const CausalParams& p, int b, int& row0, int& n, int& prefix, bool report_it) {
     int r0, r1;
     if (p.row_start) {
-        r0 = p.row_start[b];
-        r1 = p.row_start[b + 1];
+        r0 = __ldcg(p.row_start + b);
+        r1 = __ldcg(p.row_start + b + 1);
     } else {
         r0 = b * p.max_rows;
         r1 = r0 + p.max_rows;
     }
     row0 = min(max(r0, 0), p.R);
     n = min(max(min(r1, p.R) - row0, 0), p.max_rows);
-    const int raw = p.prefix_len[b], cap = p.max_pages * kAttnSlotTok;
+    const int raw = __ldcg(p.prefix_len + b), cap = p.max_pages * kAttnSlotTok;
     prefix = min(max(raw, 0), cap);
     if (report_it) {
         if (r0 < 0 || r1 > p.R || r1 - r0 > p.max_rows || r1 < r0) report(p.status, MIRROR_DEV_CHECK, 830);

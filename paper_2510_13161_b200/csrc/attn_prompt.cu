@@ -130,7 +130,8 @@ struct Ctrl {
     uint64_t turn[2];                                   // the issuing warps take turns
     uint64_t exp_turn[2][4];                            // the two softmax warps of a scheduler take turns
     Unit first;                                         // where this CTA begins
-    int first_t, n_tiles, whole, n_list;
+    int first_t, n_tiles, whole;
+    int cut, too_long;                                  // it begins inside a unit; more tiles than 31 bits count
     int makespan, ends[2];
     int scan[kThreads / 32];
     int* status;
@@ -152,16 +153,22 @@ __device__ __noinline__ void next_segment(Segment& s, const PromptParams& p, con
             s.u.tok = 0;
             if (++s.u.b == p.c.B) {
                 s.u.b = 0;
-                if (++s.u.hs == p.n_hs) { s.u.hs = 0; ++s.u.layer; }
+                if (++s.u.hs == p.n_hs) {
+                    s.u.hs = 0;
+                    if (++s.u.layer >= p.c.L) break;     // (the lengths have been changed under the call)
+                }
             }
             causal::load_request(p.c, s.u.b, s.u.row0, s.u.n, s.u.prefix, false);
         }
-        s.u.tiles = tiles_of(p, s.u.n, s.u.prefix, s.u.tok);
+        s.u.tiles = max(tiles_of(p, s.u.n, s.u.prefix, s.u.tok), 1);
     }
     fill_segment(s, p, left);
 }
 
 // ---- the plan: every CTA for itself ----------------------------------------------------------------------------
+// It is made twice as far as its inputs are concerned: ahead of the kernel in front, from whatever the lengths are then (nothing but this
+// CTA's shared memory is written), and once that kernel is through the lengths are read again: hardly ever has one changed, and then the
+// plan is made anew.  (It takes 4 us, most of them for code that runs once.)
 __device__ int block_scan(int v, int* s_warp, int* total) {              // inclusive, over the block
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -184,23 +191,24 @@ __device__ int block_scan(int v, int* s_warp, int* total) {              // incl
 struct Scratch {
     int *base, *row0, *n, *prefix;        // [B + 1], [B] each
     int *sorted, *sorted_tiles;           // [kMaxSorted]: pairs by length
+    __device__ Scratch(int* mem, int B) : base(mem + 2 * kMaxSorted), row0(base + B + 1), n(row0 + B), prefix(n + B), sorted(mem), sorted_tiles(mem + kMaxSorted) {}
 };
+// The requests' rows; has one changed?
+__device__ __forceinline__ bool load_rows(const PromptParams& p, const Scratch& x, bool report_it) {
+    bool changed = false;
+    for (int b = threadIdx.x; b < p.c.B; b += kThreads) {
+        int row0, n, prefix;
+        causal::load_request(p.c, b, row0, n, prefix, report_it);
+        changed |= x.row0[b] != row0 || x.n[b] != n || x.prefix[b] != prefix;
+        x.row0[b] = row0; x.n[b] = n; x.prefix[b] = prefix;
+    }
+    return changed;
+}
 __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* mem) {
     const int tid = threadIdx.x, lane = tid & 31, B = p.c.B, cta = blockIdx.x;
-    Scratch x;
-    x.sorted = mem;
-    x.sorted_tiles = x.sorted + kMaxSorted;
-    x.base = x.sorted_tiles + kMaxSorted;
-    x.row0 = x.base + B + 1;
-    x.n = x.row0 + B;
-    x.prefix = x.n + B;
-    for (int b = tid; b < B; b += kThreads) {
-        int row0, n, prefix;
-        causal::load_request(p.c, b, row0, n, prefix, cta == 0);
-        x.row0[b] = row0; x.n[b] = n; x.prefix[b] = prefix;
-        x.base[b + 1] = (n + 2 * p.nt - 1) / (2 * p.nt);
-    }
-    if (tid == 0) { x.base[0] = 0; ctrl->makespan = 0; ctrl->n_tiles = 0; ctrl->whole = 0; ctrl->n_list = 0; }
+    const Scratch x(mem, B);
+    for (int b = tid; b < B; b += kThreads) x.base[b + 1] = (x.n[b] + 2 * p.nt - 1) / (2 * p.nt);
+    if (tid == 0) { x.base[0] = 0; ctrl->makespan = 0; ctrl->n_tiles = 0; ctrl->whole = 0; ctrl->cut = 0; ctrl->too_long = 0; }
     __syncthreads();
     if (tid < 32) {
         int acc = 0;
@@ -217,10 +225,7 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
     }
     __syncthreads();
     const int pairs = x.base[B];
-    if (pairs == 0) {
-        if (tid == 0) p.c.begins[cta] = {0, 0, 0, 0};
-        return;
-    }
+    if (pairs == 0) return;
     auto pair = [&](int c) {                             // pair number c, in the order of the rows
         int lo = 0, hi = B - 1;                          // the first b with base[b + 1] > c
         while (lo < hi) {
@@ -246,10 +251,7 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
     const int lh = p.c.L * p.n_hs;
     const long long seq = (long long)lh * total, units = (long long)lh * pairs;
     if (seq >= (1ll << 31)) {
-        if (tid == 0) {
-            causal::report(p.c.status, MIRROR_DEV_CHECK, 833);
-            p.c.begins[cta] = {0, 0, 0, 0};
-        }
+        if (tid == 0) ctrl->too_long = 1;
         return;
     }
     const int rounds = (int)min((units + p.n_cta - 1) / p.n_cta, 1000ll);
@@ -302,7 +304,6 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
                     u.hs = l - u.layer * p.n_hs;
                     ctrl->list[tid] = u;
                     tiles = u.tiles;
-                    atomicAdd(&ctrl->n_list, 1);
                     if (tid == 0) { ctrl->first = u; ctrl->first_t = 0; }
                 }
             }
@@ -311,7 +312,6 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
                 if (lane == 0) {
                     ctrl->n_tiles = tiles;
                     ctrl->whole = 1;
-                    p.c.begins[cta] = {0, 0, 0, 0};
                 }
             }
             return;
@@ -339,21 +339,21 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
             // (this pair's tiles lie in front of both boundaries' places within their head, or hold them)
             if (x0 < seq && rem0 >= cum && rem0 < cum + mine.tiles) {
                 Unit u = mine;
-                u.layer = lh0 / p.n_hs;
-                u.hs = lh0 - u.layer * p.n_hs;
-                int t = rem0 - cum;
-                if (cta == 0) t = 0;
-                bool next = false;
+                int t = rem0 - cum, at = lh0;
                 if (t <= tol) {
                     s_ends[0] = (int)x0 - t;
                     t = 0;
-                } else if (mine.tiles - t <= tol) {
+                } else if (mine.tiles - t <= tol) {      // (to the next unit)
                     s_ends[0] = (int)x0 + mine.tiles - t;
                     t = 0;
-                    next = true;
+                    const int c = c0 + tid + 1;
+                    u = pair(c < pairs ? c : 0);
+                    at += c == pairs;
                 }
+                u.layer = at / p.n_hs;
+                u.hs = at - u.layer * p.n_hs;
                 ctrl->first = u;
-                ctrl->first_t = next ? -1 : t;
+                ctrl->first_t = t;
             }
             if (x1 < seq && rem1 >= cum && rem1 < cum + mine.tiles) {
                 const int t = rem1 - cum;
@@ -366,20 +366,7 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
     if (tid == 0) {
         const int n = s_ends[1] - s_ends[0];
         ctrl->n_tiles = n;
-        if (n > 0) {
-            if (ctrl->first_t < 0) {                     // (the boundary moved to the next unit)
-                Segment s;
-                s.u = ctrl->first;
-                s.k = 0;
-                next_segment(s, p, ctrl, n);
-                ctrl->first = s.u;
-                ctrl->first_t = 0;
-            }
-            p.firsts[cta] = ctrl->first;
-            p.c.begins[cta] = {ctrl->first_t > 0 ? 1 : 0, ctrl->first.layer, ctrl->first.row0 + ctrl->first.tok, ctrl->first.hs};
-        } else {
-            p.c.begins[cta] = {0, 0, 0, 0};
-        }
+        ctrl->cut = n > 0 && ctrl->first_t > 0;
     }
 }
 
@@ -488,14 +475,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
         ptx::tmem_alloc(&ctrl->tmem_base, kTmemCols);
         ptx::tmem_relinquish();
     }
+    const Scratch lengths((int*)ring, p.c.B);
+    load_rows(p, lengths, false);
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
+    make_plan(p, ctrl, (int*)ring);
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    make_plan(p, ctrl, (int*)ring);
+    if (__syncthreads_or(load_rows(p, lengths, blockIdx.x == 0))) make_plan(p, ctrl, (int*)ring);
     ptx::fence_proxy_async();                            // (the ring is filled by copies from here on)
     __syncthreads();
+    if (tid == 0) {
+        if (ctrl->too_long) causal::report(p.c.status, MIRROR_DEV_CHECK, 833);
+        if (!p.never_cut) {
+            const Unit& u = ctrl->first;
+            p.c.begins[blockIdx.x] = ctrl->cut ? GroupBegin{1, u.layer, u.row0 + u.tok, u.hs} : GroupBegin{0, 0, 0, 0};
+            if (ctrl->cut) p.firsts[blockIdx.x] = u;
+        }
+    }
     const uint32_t tmem_base = ctrl->tmem_base;
     const int n_tiles = ctrl->n_tiles;
     auto first_segment = [&](Segment& s) {

@@ -228,7 +228,7 @@ extern "C" mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, 
     p.half = rope ? rope->rotary_dim / 2 : 0;
     p.interleaved = rope && rope->interleaved;
     p.amplitude = rope ? (float)rope->amplitude : 1.f;
-    for (int i = 0; i < 64; ++i) p.turns[i] = rope ? rope->freq[i] / 6.283185307179586476925286766559 : 0.0;
+    for (int i = 0; i < 64; ++i) p.turns[i] = rope ? rope->freq[i] * 0.15915494309189533577 : 0.0;
     p.q_row = q_row; p.q_layer = q_layer; p.kv_row = kv_row; p.kv_layer = kv_layer; p.layer_stride = kv->layer_stride;
     p.row_start = rows->row_start; p.page_table = kv->page_table; p.prefix_len = kv->prefix_len;
     p.q = (const __nv_bfloat16*)q; p.k = (const __nv_bfloat16*)k; p.v = (const __nv_bfloat16*)v;
