@@ -380,50 +380,33 @@ struct Cfg {
     static constexpr int kQBytes = kHalves * kQHalfBytes;
 };
 
-// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM; `rows` are the stream's positions.  Returns the row's
-// maximum where it is asked for.  (Two slots at a time: most of a tile's pairs are seen by all rows, or by none.)
-__device__ __noinline__ float mask_tile(uint32_t s_addr, int slot0, const Keys& k, int pos, const StreamRows& rows, int window, int n_sink, int chunks, bool want_max) {
-    float mx = -INFINITY;
-    auto bits = [&](int slot) -> uint32_t {
-        if (slot >= k.slots) return 0u;
-        const int key0 = k.page(slot) * kSlotTok, at = pos - key0;                          // the row's own token, in the slot
-        uint32_t m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
-        if (window > 0) {
-            const int lo = at - window + 1, sk = n_sink - key0;
-            const uint32_t in = lo <= 0 ? 0xffffu : lo > 15 ? 0u : 0xffffu & ~((1u << lo) - 1u);
-            m &= in | (sk >= 16 ? 0xffffu : sk <= 0 ? 0u : (1u << sk) - 1u);
-        }
-        return m;
-    };
+// Scores of tokens that the row at position `pos` does not see become -inf, in TMEM; `rows` are the stream's positions.  A slot at a time,
+// and little code: most of a tile's slots are seen by all rows, or by none, and what runs once per unit is bound by the fetch of its
+// instructions (32 columns at a time, unrolled, with the maximum taken on the way: 4400 cycles, this and tile_max 2500).
+__device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, int slots, const Keys& k, int pos, const StreamRows& rows, int window, int n_sink) {
+    const int first_lo = window > 0 ? rows.first - window : -1, last_lo = window > 0 ? rows.last - window : -1;     // (what lies up to there is out of the window)
 #pragma unroll 1
-    for (int c = 0; c < chunks; ++c, s_addr += 32) {
-        const int a = slot0 + 2 * c;
-        uint32_t r[32];
-        const int key0 = k.page(a) * kSlotTok, key1 = k.page(min(a + 1, k.slots - 1)) * kSlotTok + kSlotTok - 1;
-        const bool none = a >= k.slots || key0 > rows.last || (window > 0 && key1 <= rows.first - window && key0 >= n_sink);
-        if (none) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) r[j] = 0xff800000u;
-            tmem_st_32x32b_x32(s_addr, r);
-            continue;
+    for (int c = 0; c < slots; ++c, s_addr += 16) {
+        const int key0 = k.page(min(slot0 + c, k.slots - 1)) * kSlotTok, key1 = key0 + kSlotTok - 1;
+        const bool there = slot0 + c < k.slots;
+        if (there && key1 <= rows.first && (key0 > last_lo || key1 < n_sink)) continue;
+        uint32_t r[16], m = 0;
+        if (there && key0 <= rows.last && (key1 > first_lo || key0 < n_sink)) {
+            ptx::tmem_ld_32x32b_x16(s_addr, r);
+            const int at = pos - key0;                                                     // the row's own token, in the slot
+            m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
+            if (window > 0) {
+                const int lo = at - window + 1, sk = n_sink - key0;
+                const uint32_t in = lo <= 0 ? 0xffffu : lo > 15 ? 0u : 0xffffu & ~((1u << lo) - 1u);
+                m &= in | (sk >= 16 ? 0xffffu : sk <= 0 ? 0u : (1u << sk) - 1u);
+            }
+            tmem_ld_wait16(r);
         }
-        const bool all = a + 1 < k.slots && key1 <= rows.first && (window == 0 || key0 > rows.last - window || key1 < n_sink);
-        if (all && !want_max) continue;
-        ptx::tmem_ld_32x32b_x32(s_addr, r);
-        const uint32_t m = all ? 0xffffffffu : bits(a) | bits(a + 1) << 16;
-        tmem_ld_wait32(r);
-        if (!all) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) r[j] = (m & (1u << j)) ? r[j] : 0xff800000u;
-            tmem_st_32x32b_x32(s_addr, r);
-        }
-        if (want_max) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(mx) : "f"(__uint_as_float(r[j])), "f"(__uint_as_float(r[j + 1])));
-        }
+        for (int j = 0; j < 16; ++j) r[j] = (m & (1u << j)) ? r[j] : 0xff800000u;
+        tmem_st_32x32b_x16(s_addr, r);
     }
     tmem_st_wait();
-    return mx;
 }
 
 // 32 bytes of a row
@@ -754,9 +737,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                     // that have been read.
                     const int halves = slots_seen(sg, rows, t) > kTileSlots / 2 ? 2 : 1;
                     // The offset is set by the first tile in which the row sees anything (before that every P was 0).
-                    const bool set_off = __any_sync(0xffffffffu, off == -INFINITY);
-                    if (!whole_tile || set_off) {
-                        const float mx = whole_tile ? tile_max(s_addr, 4) : mask_tile(s_addr, t * kTileSlots, sg.keys, pos, rows, p.c.window, p.c.n_sink, 2 * halves, set_off);
+                    if (!whole_tile) mask_tile(s_addr, t * kTileSlots, halves * (kTileSlots / 2), sg.keys, pos, rows, p.c.window, p.c.n_sink);
+                    if (__any_sync(0xffffffffu, off == -INFINITY)) {
+                        const float mx = tile_max(s_addr, 2 * halves);
                         if (off == -INFINITY) off = mx * sc;       // (-inf when nothing is visible yet)
                     }
                     float sum = 0.f;
@@ -774,11 +757,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
                         exp_chunk<false>(ra, sc2, no2, pk, s0, s1);
                         tmem_ld_wait32(rb);
                         ptx::tmem_ld_32x32b_x32(s_addr + 64, ra);    // (of no use to the second half)
-                        if (h == halves - 1 && !redone) pass_turn();
                         exp_chunk<false>(rb, sc2, no2, pk + 16, s0, s1);
                         float a, b;
                         unpack2(add2(s0, s1), a, b);
                         const float half_sum = a + b;
+                        if (h == halves - 1 && !redone) pass_turn();
                         const bool grow = half_sum > kSumLimit && !redone;
                         if (__any_sync(0xffffffffu, grow)) {
                             tmem_ld_wait32(ra);
