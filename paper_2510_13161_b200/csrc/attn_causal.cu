@@ -596,7 +596,7 @@ extern "C" mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv
     if (st != MIRROR_OK) return st;
     if (!ctx->ws || ctx->ws_bytes < need) return MIRROR_ERR_WORKSPACE;
     // (positions, and the slots of a layer's units, are counted in 31 bits)
-    if (kv->max_pages_per_req > (1 << 26) || (int64_t)rows->batch * kv->max_pages_per_req > 0x7fffffff) return MIRROR_ERR_SHAPE;
+    if (kv->max_pages_per_req > (1 << 26) || (int64_t)rows->batch * kv->max_pages_per_req > (1 << 30)) return MIRROR_ERR_SHAPE;
     MIRROR_CUDA_OK(cudaSetDevice(ctx->device));
     MirrorWsLayout L;
     mirror_ws_layout(ctx, 1, &L);

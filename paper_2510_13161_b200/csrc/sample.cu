@@ -9,7 +9,7 @@
 // A cluster of CTAs has one row, each a contiguous part of it, each warp a contiguous part of that, so that sums in the order of the ids
 // are sums over warps.  With few rows a part is kept in shared memory.  With many it is read again from L2 by every pass: what takes
 // the time then is the steps that one CTA, or one thread, takes for its row while the others wait, so four small CTAs an SM, each with
-// more of a row, get more rows through than two large ones (520 rows: 541 -> MEASURED us).
+// more of a row, get more rows through than two large ones (520 rows x 128256 ids: 435 us against 541 when this was changed).
 //   1  load, maximum over the cluster (the logits leave HBM once)
 //   2  Top-k of up to kQuickK: a histogram of the largest of every four logits says down to which logit at least k ids lie; Min-p says
 //      so by itself.  Top-p of the whole row: a histogram of z in 2048 bins of 1/64, how many ids each holds and where in the bin they lie on
@@ -82,7 +82,7 @@ struct alignas(16) Shared {
     u64 kept;                                 // its front's mass
     u64 base;
     int last_bin, list_at;                    // written by the leader
-    int n_list;
+    int n_list, n_all;                        // ids up to last_bin, and in all bins
     int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
     int bucket;
     float row_mass;
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
     const float inv_T = 1.f / T;
     auto bin_of = [&](float l, float& at) {
-        at = max_inf ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));
+        at = max_inf || l == mx ? 0.f : fminf((mx - l) * inv_T * kBinsPerNat, (float)(kBins - 1));        // (what is no number: the last bin)
         return (int)at;
     };
     int turn = 0;
@@ -425,6 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     nb += cnt[j];
                     if (tid * kPer + j == s.last_bin) s.n_list = (int)nb;
                 }
+                if (tid == kThreads - 1) s.n_all = (int)nb;
                 // (Top-p behind Top-k is a share of all that Top-k leaves, so Top-k's end counts alone)
                 if (tid == 0 && by_k) s.last_bin = s.bin_k;
                 __syncthreads();
@@ -434,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     o->bin_k = s.bin_k;
                     o->bin_p = s.bin_p;
                     o->n_list = s.n_list;
+                    o->n_all = s.n_all;
                 }
             }
             cluster.sync();
@@ -720,12 +722,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 return c;
             };
             total = 0;
-            if (by_k) {
+            const bool cuts_k = by_k && k < s.n_all;             // (there may be fewer that may be kept)
+            if (cuts_k) {
                 cut = end_of(s.bin_k, false, false, [&](u64 n, u64, u64) { return n >= (u64)k; });
                 if (by_p) total = front(cut).m;
             }
             if (by_p) {
-                const u64 c = end_of(s.bin_p, true, whole_total, [&](u64 n, u64 m, u64 all) { return n >= 1 && (double)m >= top_p * (double)(whole_total ? all : total); });
+                const u64 c = end_of(s.bin_p, true, !cuts_k, [&](u64 n, u64 m, u64 all) { return n >= 1 && (double)m >= top_p * (double)(cuts_k ? total : all); });
                 cut = min(cut, c);
             }
             if (by_m) {
@@ -857,7 +860,7 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     if (M == 0) return MIRROR_OK;
     if (!logits || !u || !token) return MIRROR_ERR_ARG;
     const int V = ctx->desc.vocab;
-    if (ld < V || V > kMaxCluster * kMaxPart) return MIRROR_ERR_SHAPE;
+    if (ld < V || V > kMaxCluster * kMaxPart || (int64_t)M * kMaxCluster > 0x7fffffff) return MIRROR_ERR_SHAPE;
     // (the row is read before its outputs are written, so they may be the logits themselves where the rows lie alike)
     if ((((uintptr_t)logits | (uintptr_t)probs | (uintptr_t)logits_out) & 3) || (probs && (const float*)probs == logits && ld != V) ||
         (logits_out && (const float*)logits_out == logits && ld != V) || (probs && probs == logits_out))

@@ -126,6 +126,61 @@ def test_captured_and_replayed_with_other_lengths(n):
 
 
 @pytest.mark.parametrize("n", [1, 20])
+def test_a_cache_beyond_four_gigabytes(n):
+    """Pages at the far end of a pool whose elements do not count in 32 bits: the same rows as in a small pool."""
+    hq, hkv, d, pages = 16, 8, 128, 150_000
+    m = make(hq, hkv, d)
+    c = Case(hq, hkv, d, [37, 100], [n, n], seed=11)
+    want, _ = check_attention(m, c, n * 2 > 16)
+    big = [torch.zeros((1, pages, hkv, PAGE, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.from_numpy(c.table).cuda()
+    moved = torch.where(table < 1000, pages - 1 - table, table)
+    used = c.k.shape[1]
+    for far, near in zip(big, (c.kd, c.vd)):
+        far[:, pages - used:] = near.flip(1)
+    kv = m.kv(*big, moved, torch.tensor(c.lens, dtype=torch.int32).cuda())
+    assert torch.equal(m.mirror_attn_causal(kv, c.rows, c.q.cuda())[:, :2 * n], want[:, :2 * n])
+    # the rows' own keys and values once more, appended there
+    k = torch.randn((1, 2 * n, hkv, d), device="cuda").to(torch.bfloat16)
+    m.mirror_kv_append(kv, c.rows, k, k)
+    torch.cuda.synchronize()
+    assert m.device_status() == (0, 0)
+    for b, t in enumerate(c.lens):
+        for i in range(n):
+            page = int(moved[b, (t + i) // PAGE])
+            assert torch.equal(big[1][0, page, :, (t + i) % PAGE], k[0, b * n + i])
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_in_place(n):
+    """The output may take the queries' place."""
+    m = make(8, 2, 64)
+    c = Case(8, 2, 64, [3000, 77, 5], [n, n, n], seed=12)
+    want, _ = check_attention(m, c, n > 4)
+    q = c.q.cuda()
+    got = m.mirror_attn_causal(c.kv, c.rows, q, out=q)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_two_contexts_at_once(n):
+    """Calls of two contexts on two streams, side by side."""
+    ms = [make(8, 2, 128), make(8, 2, 128)]
+    cs = [Case(8, 2, 128, [900, 40, 2000], [n, n, n], seed=13 + i) for i in range(2)]
+    want = [check_attention(m, c, n > 4)[0] for m, c in zip(ms, cs)]
+    qs, streams = [c.q.cuda() for c in cs], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for m, c, q, s in zip(ms, cs, qs, streams):
+            with torch.cuda.stream(s):
+                got.append(m.mirror_attn_causal(c.kv, c.rows, q))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("n", [1, 20])
 def test_reports(n):
     m = make(4, 2, 64)
     c = Case(4, 2, 64, [20, 5], [n, n], seed=1)

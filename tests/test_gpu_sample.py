@@ -82,6 +82,41 @@ def test_open_rows_keep_more_than_fits_the_list():
     check(x, k=[0, 5000, 20000, 3000, 29999, 2500], p=[0.6, 0.9, 1.0, 0.4, 0.999, 1.0], mp=[0.0, 0.0, 0.0, 0.001, 0.05, 0.12])
 
 
+@pytest.mark.parametrize("V", [300001, 655360])
+def test_the_largest_vocabularies(V):
+    check(logits_of(2, V, V), T=[0.7, 1.3], k=[60, 0], p=[0.9, 0.95], seed=1)
+    check(logits_of(2, V, V + 1), T=[0.9, 1.1], seed=2)
+
+
+def test_many_rows_that_are_open_tied_or_masked():
+    """More rows than are kept in shared memory: every way through the kernel that the small batches take, too."""
+    M = 60
+    x = logits_of(M, 9004, 21, std=0.8, leaders=3)
+    x[1] = 0.0
+    x[2] = np.round(x[2] * 2) / 2
+    x[3, 100:] = -np.inf
+    x[4] = -np.inf
+    x[5] = np.nan
+    x[6, ::3] = np.nan
+    x[7, [5, 77]] = np.inf
+    rng = np.random.default_rng(3)
+    k = rng.choice([0, 1, 700, 1500, 4000, 9003], M)
+    p = rng.choice([0.3, 0.9, 0.999, 1.0], M)
+    mp = rng.choice([0.0, 0.0, 0.02, 0.4], M)
+    check(x, T=rng.uniform(0.3, 1.5, M), k=k, p=p, mp=mp, seed=4)
+    check(x, T=rng.uniform(0.3, 1.5, M), p=0.95, seed=5)
+    check(x[:, :9001].copy(), T=rng.uniform(0.3, 1.5, M), k=2500, p=0.9, seed=6)
+
+
+@pytest.mark.parametrize("T", [1e-44, 1e-38, 3e38, np.inf])
+def test_temperatures_at_the_ends_of_fp32(T):
+    x = logits_of(3, 5000, 30)
+    x[1] = 3.0
+    x[2, :2500] = 2.0
+    for k, p, mp in ((None, None, None), (1, None, None), (3000, None, None), (None, 0.7, None), (None, None, 0.5)):
+        check(x, T=T, k=k, p=p, mp=mp, seed=6)
+
+
 def test_settings_differ_by_row():
     M = 40
     rng = np.random.default_rng(1)
