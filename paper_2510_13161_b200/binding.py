@@ -237,7 +237,8 @@ class Mirror:
         self.device = torch.device("cuda", device)
         self._ctx = C.c_void_p()
         _check(self.lib.mirror_create(C.byref(self._ctx), C.byref(self.desc), device), "mirror_create")
-        self._heads = (n_q_heads, n_kv_heads, head_dim)
+        self._heads, self._vocab = (n_q_heads, n_kv_heads, head_dim), vocab
+        self._rows_need = None
         self._ws = None
         self._need = {}              # workspace bytes by (what, batch, nodes): they depend on nothing else
         self._keep = []
@@ -517,14 +518,11 @@ class Mirror:
             out = torch.empty_like(q)
         if q.shape != shape or out.shape != shape or (lse_out is not None and lse_out.shape != shape[:3]):
             raise ValueError(f"q and out must be {shape}, lse_out {shape[:3]}")
-        key = ("rows", rows.batch, rows.n_rows)
-        need = self._need.get(key)
+        need = self._rows_need               # (the same for all rows of a context)
         if need is None:
             n = C.c_size_t()
             _check(self.lib.mirror_rows_workspace_bytes(self._ctx, C.byref(rows), C.byref(n)), "mirror_rows_workspace_bytes")
-            need = n.value
-            if len(self._need) < 4096:
-                self._need[key] = need
+            need = self._rows_need = n.value
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             _check(self.lib.mirror_set_workspace(self._ctx, C.c_void_p(self._ws.data_ptr()), need), "mirror_set_workspace")
@@ -539,24 +537,30 @@ class Mirror:
         """One token of each row of logits fp32 [M, V] (rows may be strided) from uniforms u [M], under per-row filters (tensors [M], None: off).
         probs: the filtered distribution, q_probs of accept_in; logits: what mirror_accept_select takes as a target's, with an lse of zeros."""
         M, V = logits.shape
-        if V != self.desc.vocab:
-            raise ValueError(f"logits must have {self.desc.vocab} columns, got {V}")
-        if not logits.is_cuda or logits.dtype is not torch.float32 or (V > 1 and logits.stride(1) != 1):
+        if V != self._vocab:
+            raise ValueError(f"logits must have {self._vocab} columns, got {V}")
+        ld, one = logits.stride()
+        if not logits.is_cuda or logits.dtype is not torch.float32 or (V > 1 and one != 1):
             raise ValueError("logits must be a CUDA tensor of torch.float32 with contiguous rows")
-        for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
-            if t is not None and t.numel() != M:
+
+        def per_row(t, dtype, name):
+            if t is None:
+                return None
+            if t.numel() != M:
                 raise ValueError(f"{name} must have {M} entries")
-        dev = logits.device
-        res = dict(token=torch.empty(M, dtype=torch.int32, device=dev), n_kept=torch.empty(M, dtype=torch.int32, device=dev),
-                   logprob=torch.empty(M, dtype=torch.float32, device=dev),
-                   probs=torch.empty((M, V), dtype=torch.float32, device=dev) if want_probs else None,
-                   logits=torch.empty((M, V), dtype=torch.float32, device=dev) if want_logits else None)
-        _check(self.lib.mirror_sample(self._ctx, logits.data_ptr(), logits.stride(0) if M > 1 else V, M,
-                                      _ptr(temperature, torch.float32, "temperature"), _ptr(top_k, torch.int32, "top_k"),
-                                      _ptr(top_p, torch.float32, "top_p"), _ptr(min_p, torch.float32, "min_p"), _ptr(u, torch.float32, "u"),
-                                      _ptr(res["token"]), _ptr(res["logprob"]), _ptr(res["n_kept"]), _ptr(res["probs"]),
-                                      _ptr(res["logits"]), _stream(stream)), "mirror_sample")
-        return res
+            return _ptr(t, dtype, name)
+        f32, dev = torch.float32, logits.device
+        args = (per_row(temperature, f32, "temperature"), per_row(top_k, torch.int32, "top_k"), per_row(top_p, f32, "top_p"), per_row(min_p, f32, "min_p"),
+                per_row(u, f32, "u"))
+        token = torch.empty(M, dtype=torch.int32, device=dev)
+        n_kept = torch.empty(M, dtype=torch.int32, device=dev)
+        logprob = torch.empty(M, dtype=f32, device=dev)
+        probs = torch.empty((M, V), dtype=f32, device=dev) if want_probs else None
+        target = torch.empty((M, V), dtype=f32, device=dev) if want_logits else None
+        _check(self.lib.mirror_sample(self._ctx, logits.data_ptr(), ld if M > 1 else V, M, *args, token.data_ptr(), logprob.data_ptr(), n_kept.data_ptr(),
+                                      None if probs is None else probs.data_ptr(), None if target is None else target.data_ptr(), _stream(stream)),
+               "mirror_sample")
+        return dict(token=token, n_kept=n_kept, logprob=logprob, probs=probs, logits=target)
 
     # ---- the target's layers around the attention ---------------------------------------------
     def target(self, layers: Sequence[dict], norm_final: torch.Tensor, intermediate: int, rope_theta: float = 1e6,

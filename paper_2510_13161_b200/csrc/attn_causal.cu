@@ -547,7 +547,7 @@ mirror_status token_launch(mirror_ctx* ctx, const mirror_kv* kv, const CausalPar
     const int ctas = ctx->num_sms * std::max(1, std::min((int)C::kCtas, (int)(kSmemPerSm / (smem + 1024))));
     static_assert(sizeof(attn::GroupBegin) == 16, "notes");
     if (ctas > kMaxCtas || (size_t)ctas * 2 * C::kRec * sizeof(float) > records_bytes) return MIRROR_ERR_SHAPE;
-    MIRROR_CUDA_OK(cudaFuncSetAttribute(attn_token_kernel<D, kWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    MIRROR_CUDA_OK(mirror_allow_smem(ctx, kRowsToken + (D == 128) + (kWarps > 4 ? 2 : 0), attn_token_kernel<D, kWarps>, 232448));
     MIRROR_CUDA_OK(mirror_launch_pdl(attn_token_kernel<D, kWarps>, dim3((unsigned)ctas), dim3(C::kThreads), smem, stream, tm, p, never_cut));
     ctx->launches += 1;
     if (!never_cut) {

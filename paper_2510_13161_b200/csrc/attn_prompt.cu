@@ -910,12 +910,12 @@ mirror_status mirror_attn_prompt_launch(mirror_ctx* ctx, const mirror_kv* kv, co
         using C = decltype(cfg);
         const size_t fixed = 2 * (size_t)C::kQBytes + kCtrlBytes;
         const int stages = std::min((int)((kSmemLimit - fixed) / C::kStageBytes), kMaxStages);
-        MIRROR_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit));
+        MIRROR_CUDA_OK(mirror_allow_smem(ctx, kRowsPrompt + (D == 128), kern, (int)kSmemLimit));
         MIRROR_CUDA_OK(mirror_launch_pdl(kern, dim3((unsigned)p.n_cta), dim3(kThreads), fixed + (size_t)stages * C::kStageBytes, stream, tm, p, stages));
         ctx->launches += 1;
         if (p.never_cut) return MIRROR_OK;
         constexpr int kSmem = merge_smem(kMergeSlotsPrompt);
-        MIRROR_CUDA_OK(cudaFuncSetAttribute(merge, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        MIRROR_CUDA_OK(mirror_allow_smem(ctx, kRowsPromptMerge + (D == 128), merge, kSmem));
         MIRROR_CUDA_OK(mirror_launch_pdl(merge, dim3((unsigned)(p.n_cta - 1), 2), dim3(kMergeThreads), kSmem, stream, p));
         ctx->launches += 1;
         return MIRROR_OK;

@@ -59,6 +59,7 @@ struct mirror_ctx {
     long long launches = 0;
     bool lm_attr_set = false;
     bool lm_pair_attr_set = false;
+    unsigned rows_attr_set = 0;                             // a bit for each kernel of the calls on rows without a tree (MirrorRowsKernel)
     cudaEvent_t stage_ev[4] = {nullptr, nullptr, nullptr, nullptr};
     bool stage_ev_on = false;
     cudaStream_t copy_stream = nullptr;                     // mirror_verify_step_host: created on first use
@@ -486,6 +487,16 @@ struct E4m3Scale {
         return copysignf(fmaf(fmaf(-t, s, x), inv, t), x);                 // (a zero keeps its sign)
     }
 };
+
+// A kernel's attributes, set on its first launch through a context (setting them takes 0.6 us).
+enum MirrorRowsKernel { kRowsToken = 0, kRowsPrompt = 4, kRowsPromptMerge = 6, kRowsSample = 8 };
+template <class Kernel>
+inline cudaError_t mirror_allow_smem(mirror_ctx* ctx, int bit, Kernel kernel, int bytes) {
+    if (ctx->rows_attr_set >> bit & 1u) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) ctx->rows_attr_set |= 1u << bit;
+    return e;
+}
 
 template <typename... KArgs, typename... Args>
 inline cudaError_t mirror_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,

@@ -895,8 +895,12 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     p.off_shift = p.part <= 16384 ? 17 : 16;
     const size_t smem = sizeof(Shared) + (resident ? (size_t)p.part * sizeof(float) : 0);
     auto kernel = resident ? sample_kernel<true, 512> : sample_kernel<false, 256>;
-    MIRROR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    if (C > 8) MIRROR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    const int bit = kRowsSample + (resident ? 2 : 0);
+    MIRROR_CUDA_OK(mirror_allow_smem(ctx, bit, kernel, (int)(sizeof(Shared) + (resident ? 16384 * sizeof(float) : 0))));
+    if (C > 8 && !(ctx->rows_attr_set >> (bit + 1) & 1u)) {
+        MIRROR_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        ctx->rows_attr_set |= 1u << (bit + 1);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)C * (unsigned)M);
     cfg.blockDim = dim3((unsigned)threads);
