@@ -62,6 +62,8 @@ struct SampleParams {
     int32_t* n_kept;
     float* probs;
     float* logits_out;
+    double two_s, two_ms;                     // 2^S, 2^-S
+    double table[kTable];                     // 2^(j / 16)
 };
 
 struct Sums {
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
     auto load = [&](int i) -> float4 { return kResident ? *reinterpret_cast<const float4*>(z + i) : fetch(i); };
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
-    if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
+    if (tid < kTable) s.table[tid] = p.table[tid];
 #pragma unroll
     for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     if (lane == 0) s.warp_sum[warp][0] = __float_as_uint(mx);
@@ -288,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ids that may be kept: neither NaN nor -inf, and where the maximum is +inf only those
     const float least = max_inf ? INFINITY : -3.4028235e38f;
     auto may = [&](float l) { return l >= least; };
-    const u64 min_w = by_m ? (u64)fmin(ceil(min_p * exp2((double)p.shift)), exp2((double)p.shift)) : 0ull;
+    const u64 min_w = by_m ? (u64)fmin(ceil(min_p * p.two_s), p.two_s) : 0ull;
     // composite key of an id: smaller is ahead
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
     const float inv_T = 1.f / T;
@@ -478,11 +480,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         };
         float from = least;
         int n_list = kList + 1;
-        const bool quick = by_k ? k <= kQuickK : by_m && !by_p;
+        const bool all = p.V <= kList;                           // (then the list takes the row)
+        const bool quick = all || (by_k ? k <= kQuickK : by_m && !by_p);
         // ---- 2: histograms.  A word counts in its upper bits and sums in its lower ones in which part of the bin the ids lie: neither half
         // outgrows its bits over a part's ids.
         if (quick) {
-            if (by_k) {
+            if (by_k && k == 1) {
+                from = mx;
+            } else if (by_k && !all) {
                 for (int i = w0 + lane * 4; i < w1; i += 128) {
                     const float4 v = load(i);
                     const float top = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
@@ -494,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             }
             if (!(by_k && by_p)) from = fmaxf(from, below_m);
             from = from >= least ? from : least;
-            n_list = push(from, false);
+            n_list = push(from, whole_total);
         }
         if (n_list > kList) {
             __syncthreads();
@@ -604,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 }
                 if (!p.probs && !p.logits_out) return;
                 cluster.sync();                                  // (the rows are filled)
-                const double unit = (double)Z * exp2(-(double)p.shift), inv = 1.0 / unit, ln_z = log(unit);
+                const double unit = (double)Z * p.two_ms, inv = 1.0 / unit, ln_z = log(unit);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
                     if (tid * kPer + j >= n) break;
@@ -815,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         }
     }
     if (p.probs || p.logits_out) {
-        const double unit = (double)Z * exp2(-(double)p.shift), inv = 1.0 / unit, ln_z = log(unit);
+        const double unit = (double)Z * p.two_ms, inv = 1.0 / unit, ln_z = log(unit);
         float* const probs = p.probs ? p.probs + (size_t)row * p.V + first : nullptr;
         float* const lg = p.logits_out ? p.logits_out + (size_t)row * p.V + first : nullptr;
         for (int i = w0 + lane * 4; i < w1; i += 128) {
@@ -872,6 +877,9 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
     while ((1ll << bits) < V) ++bits;
     p.shift = 62 - bits < 51 ? 62 - bits : 51;                   // (a weight has to fit a double's 52 bits)
     p.id_shift = bits > 11 ? bits - 11 : 0;
+    p.two_s = ldexp(1.0, p.shift);
+    p.two_ms = ldexp(1.0, -p.shift);
+    for (int j = 0; j < kTable; ++j) p.table[j] = exp2((double)j / kTable);
     p.temperature = ctx->temperature;
     p.logits = logits; p.temperatures = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p; p.u = u;
     p.token = token; p.logprob = logprob; p.n_kept = n_kept; p.probs = probs; p.logits_out = logits_out;
