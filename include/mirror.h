@@ -367,11 +367,14 @@ mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, const mirro
  * visible).
  *   q, out    bf16 [L, R, Hq, d] contiguous (q already turned): out = softmax(scale q k^T over the visible tokens) v
  *   lse_out   fp32 [L, R, Hq], nullable: natural-log softmax denominator
+ *   out may be q
  * Pages that hold no visible token are not touched (their table entries may be anything), and what lies in a touched page beside
  * the tokens that some row of its request sees may be anything, infinities and NaN included.
  * Needs a workspace of mirror_rows_workspace_bytes().  Requests of few rows (max_rows * Hq / Hkv <= 16) stream the cache through
  * warps; longer ones run on the tensor cores in tiles of 128 rows.  Rows whose positions lie beyond max_pages_per_req*16 are
- * left as they are and reported through mirror_device_status, as are lengths below 0 and pages outside the pool. */
+ * left as they are and reported through mirror_device_status, as are requests of a length below 0 and all rows of a call whose keys, over
+ * layers, heads and requests, make more tiles of 128 than 31 bits count; a page outside the pool is reported, and its tokens are read as
+ * page 0's. */
 mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, const mirror_rows* rows, size_t* bytes);
 mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mirror_rows* rows, int window, int n_sink,
                                  const void* q, void* out, float* lse_out, void* stream);
@@ -389,10 +392,11 @@ mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mir
  *   probs       fp32 [M, V], nullable: the kept tokens' probabilities, 0 elsewhere -- q_probs of mirror_accept_in for a draft
  *   logits_out  fp32 [M, V], nullable: T_ctx * ln of them, -inf elsewhere -- with an lse of zeros, the logits that
  *               mirror_accept_select takes for a target under the same filters
- * All three filters keep a front of the ranks (logit descending, id ascending), at least the first.  NaN logits are never kept (a row without
- * any other: token -1, logprob -inf, n_kept 0, probs 0), -inf only where top_k reaches them, never drawn; logits of +inf share all the mass.
- * Weights exp((logit - max) / T) are summed as 64-bit integers, scaled to 2^62 / V: sums are the same in any order.
- * One kernel, no workspace. */
+ * All three filters keep a front of the ranks (logit descending, id ascending), at least the first.  NaN and -inf are never kept (a row of
+ * nothing else: token -1, logprob -inf, n_kept 0, probs 0, logits_out -inf); logits of +inf share all the mass, and nothing else stays.
+ * Weights exp((logit - max) / T) are summed as 64-bit integers, of which 1 has at most 2^62 / V of steps: sums are the same in any order.  An id
+ * whose weight rounds to 0 steps is kept where the filters keep it, with probability 0, and never drawn.
+ * One of probs and logits_out may be logits itself where ld == V; else none of the three may overlap.  At most 655360 ids (MIRROR_ERR_SHAPE).  One kernel, no workspace. */
 mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int64_t ld, int M, const float* temperature,
                             const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token,
                             float* logprob, int32_t* n_kept, float* probs, float* logits_out, void* stream);

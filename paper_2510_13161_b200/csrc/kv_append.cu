@@ -8,6 +8,8 @@
 //
 // What bounds it: bytes (2 * rows * (Hq + 2 Hkv) * d * 2), and for single tokens the launch.  A thread moves 16 elements of a head at a time,
 // either 8 pairs or 16 elements that only pass through: two 16-byte loads and stores.
+// Measured on a B200: 5.6 TB/s over prompts of 11 k rows (0.45 GB: 80 us), 3.5 us for a token.  Tried and no faster: two or four items
+// of a thread on the way at once, eight rows or 512 threads to a block (79.5 to 97 us).
 #include <math.h>
 
 #include "mirror_internal.h"

@@ -3,7 +3,7 @@
 // With z = (logit - max) / T the weight of an id is exp(z).  Each filter keeps a front of the ranks (logit descending, id ascending), so
 // the kept set is the shortest of three fronts, and no sort of the row is needed: only where the front ends has to be found.  What
 // decides are sums of weights, and a sum that is off by 10^-7 moves the end of a Top-p front by an id in one row of a hundred (an id's
-// share is 10^-5 where the row is open).  Weights are therefore 64-bit integers, round(exp(z) 2^S) with S = 62 - ceil(log2 V), from a
+// share is 10^-5 where the row is open).  Weights are therefore 64-bit integers, round(exp(z) 2^S) with S = 62 - ceil(log2 V) (at most 51), from a
 // double-precision exponential: their sums are exact, and the same in whatever order threads and CTAs take them.
 //
 // A cluster of CTAs has one row, each a contiguous part of it, each warp a contiguous part of that, so that sums in the order of the ids
@@ -11,7 +11,8 @@
 // the time then is the steps that one CTA, or one thread, takes for its row while the others wait, so four small CTAs an SM, each with
 // more of a row, get more rows through than two large ones (520 rows x 128256 ids: 435 us against 541 when this was changed).
 //   1  load, maximum over the cluster (the logits leave HBM once)
-//   2  Top-k of up to kQuickK: a histogram of the largest of every four logits says down to which logit at least k ids lie; Min-p says
+//   2  (rows of up to kList ids go to 4 as they are, Top-k of one asks for the maximum alone)
+//      Top-k of up to kQuickK: a histogram of the largest logits of groups of 16 (or of every four, where groups are few) says down to which logit at least k ids lie; Min-p says
 //      so by itself.  Top-p of the whole row: a histogram of z in 2048 bins of 1/64, how many ids each holds and where in the bin they lie on
 //      average, packed in one word, which gives a bin's mass to 10^-3
 //   3  the leading CTA adds the histograms up and reads off the bin in which each filter's front ends, Top-p's by estimate
@@ -21,7 +22,9 @@
 //      of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
 //   5  the drawn token, by the warps' masses, and the filtered distribution
 // What bounds it: double-precision arithmetic (18 operations an id, 64 a cycle and SM) where Top-p or a draw takes the whole row, the
-// bytes otherwise; for a row alone the cluster's barriers and code that runs once.
+// bytes otherwise; for a row alone the cluster's barriers and code that runs once.  Measured on a B200: one row of 152064 ids under all
+// three filters 16.7 us (0.1 us of bytes); 64 rows x 128256 under Top-p 0.9, probabilities written, 109 us; 520 rows x 128256 under Top-k 1000
+// and Top-p 0.98, logits written, 289 us (1.85 TB/s).
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -38,9 +41,11 @@ constexpr int kBins = 2048;
 constexpr float kBinsPerNat = 64.f;
 constexpr int kList = 2048;                   // candidates that the leader ranks
 constexpr int kMaxCluster = 16;
+constexpr int kGroup = 4;                     // a group: this many of a thread's loads, 16 ids
 constexpr int kTable = 16;
 constexpr int kQuickK = 1400;                 // (the largest of every four: hardly more than k candidates then)
 constexpr int kMaxPart = 40960;               // ids of a CTA
+static_assert(kMaxPart / (4 * kGroup) <= 2 * kList && kMaxPart % (1024 * kGroup) == 0, "a part's groups have their place");
 static_assert(kBins == kList, "a thread has as many bins as candidates");
 
 struct SampleParams {
@@ -94,7 +99,10 @@ struct alignas(16) Shared {
         Drawn drawn[kBins / 4];               // (the candidates that the draw has to look at one by one)
     };
     u64 list[kList];                          // composite keys: ~order key, id; then the masses of buckets of ids
-    u64 ranked[kList];                        // the same in the order of the ranks
+    union {
+        u64 ranked[kList];                    // the same in the order of the ranks
+        float tops[2 * kList];                // (before there is a list) the largest logit of every group
+    };
 };
 static_assert(sizeof(Shared) % 16 == 0, "the logits behind it are read 16 bytes at a time");
 
@@ -228,6 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ---- 1: load, maximum.  (What cannot be kept, NaN and the part's end, becomes -inf.)
     const float* const in = p.logits + (long long)row * p.ld + first;
     float mx = -INFINITY;
+    auto numbers = [](float4 v) { return make_float4(v.x == v.x ? v.x : -INFINITY, v.y == v.y ? v.y : -INFINITY, v.z == v.z ? v.z : -INFINITY, v.w == v.w ? v.w : -INFINITY); };
     auto fetch = [&](int i) -> float4 {                          // four ids' logits from memory
         float v[4];
         if (p.vec_in && i + 4 <= n_mine) {
@@ -236,15 +245,45 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = i + j < n_mine ? in[i + j] : -INFINITY;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = v[j] == v[j] ? v[j] : -INFINITY;
-        return make_float4(v[0], v[1], v[2], v[3]);
+        return numbers(make_float4(v[0], v[1], v[2], v[3]));
     };
-#pragma unroll 8
-    for (int i = w0 + lane * 4; i < w1; i += 128) {
-        const float4 v = fetch(i);
-        mx = fmaxf(fmaxf(mx, fmaxf(v.x, v.y)), fmaxf(v.z, v.w));
-        if (kResident) *reinterpret_cast<float4*>(z + i) = v;
+    const int n_groups = (per_warp + kGroup * 128 - 1) / (kGroup * 128);          // of a thread: kGroup of its loads each
+    float* const tops = s.tops + warp * n_groups * 32 + lane;
+    auto take_group = [&](int g, const float4 (&v)[kGroup]) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const int i = w0 + (g * kGroup + j) * 128 + lane * 4;
+            if (kResident && i < w1) *reinterpret_cast<float4*>(z + i) = v[j];
+            top = fmaxf(fmaxf(top, fmaxf(v[j].x, v[j].y)), fmaxf(v[j].z, v[j].w));
+        }
+        tops[g * 32] = top;
+        mx = fmaxf(mx, top);
+    };
+    int g0 = 0;
+    if (p.vec_in) {                                              // (groups within the part: two on the way at once)
+        const int n_whole = max(0, min(w1, n_mine & ~3) - w0) / (kGroup * 128);
+        for (; g0 + 2 <= n_whole; g0 += 2) {
+            float4 v[2][kGroup];
+#pragma unroll
+            for (int j = 0; j < 2 * kGroup; ++j) {
+                const float4* const at = reinterpret_cast<const float4*>(in + w0 + (g0 * kGroup + j) * 128 + lane * 4);
+                v[j / kGroup][j % kGroup] = kResident ? __ldcs(at) : *at;
+            }
+#pragma unroll
+            for (int j = 0; j < 2 * kGroup; ++j) v[j / kGroup][j % kGroup] = numbers(v[j / kGroup][j % kGroup]);
+            take_group(g0, v[0]);
+            take_group(g0 + 1, v[1]);
+        }
+    }
+    for (; g0 < n_groups; ++g0) {
+        float4 v[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const int i = w0 + (g0 * kGroup + j) * 128 + lane * 4;
+            v[j] = i < w1 ? fetch(i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        }
+        take_group(g0, v);
     }
     auto load = [&](int i) -> float4 { return kResident ? *reinterpret_cast<const float4*>(z + i) : fetch(i); };
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
@@ -446,37 +485,79 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         const float slack = fabsf(weigh.hi) * 1e-6f;
         auto below_bin = [&](int b) { return b >= kBins - 1 || max_inf ? least : weigh.hi - (float)(b + 1) * T * (1.00002f / kBinsPerNat) - slack; };
         const float below_m = by_m && !max_inf ? weigh.hi + T * (logf((float)fmin(min_p, 1.0)) * 1.00002f - 1e-5f) - slack : least;
+        // Candidates: into the CTA's own list (an atomic of another CTA's memory is a trip of a thousand cycles), and once the exchange has
+        // told how many every CTA has, count(c) of them, one behind the other into the leader's.
+        auto gather = [&](auto count) {
+            if (rank != 0) {
+                int at = 0;
+                for (int c = 0; c < rank; ++c) at += count(c);
+                const int n = count(rank);
+                for (int i = tid; i < n; i += kThreads) lead->list[at + i] = s.list[i];
+            }
+            cluster.sync();
+        };
         // ---- 4: the ids from `from` on to the leader, and (of_all) the mass of all.  How many they are:
         u64 total = 0;
         auto push = [&](float from, bool of_all) -> int {
-            if (rank == 0 && tid == 0) s.list_at = 0;
-            cluster.sync();
-            Sums a = {0, 0, 0, 0};
-            for (int i = w0 + lane * 4; i < w1; i += 128) {
-                const float4 v4 = load(i);
-                const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-                if (of_all) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (may(v[j])) a.m += weigh(v[j]);
+            if (tid == 0) s.list_at = 0;
+            __syncthreads();
+            u64 m = 0;
+            if (of_all)
+                for (int i = w0 + lane * 4; i < w1; i += 128) {
+                    const float4 v = load(i);
+                    if (may(v.x)) m += weigh(v.x);
+                    if (may(v.y)) m += weigh(v.y);
+                    if (may(v.z)) m += weigh(v.z);
+                    if (may(v.w)) m += weigh(v.w);
                 }
-                if (fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= from) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (v[j] >= from) {
-                            ++a.n;
-                            const int slot = atomicAdd(&lead->list_at, 1);
-                            if (slot < kList) lead->list[slot] = key_of(v[j], first + i + j);
-                        }
-                }
+            // groups that have such ids, in the place of their largest logits, then a lane to a group
+            int* const groups = reinterpret_cast<int*>(tops - lane);
+            int n_hit = 0;
+            for (int g = 0; g < n_groups; ++g) {
+                const bool hit = tops[g * 32] >= from;
+                const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+                if (hit) groups[n_hit + __popc(hits & ((1u << lane) - 1u))] = w0 + g * (kGroup * 128) + lane * 4;
+                n_hit += __popc(hits);
             }
+            __syncwarp();
+            int n = 0;
+            for (int q = 0; q < n_hit; q += 32) {
+                const int i0 = q + lane < n_hit ? groups[q + lane] : w1;
+                float v[4 * kGroup];
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j)
+                    *reinterpret_cast<float4*>(v + 4 * j) = i0 + j * 128 < w1 ? load(i0 + j * 128) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                int mine = 0;
+#pragma unroll
+                for (int j = 0; j < 4 * kGroup; ++j) mine += v[j] >= from;
+                int in = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int t = __shfl_up_sync(0xffffffffu, in, o);
+                    if (lane >= o) in += t;
+                }
+                int at = 0;
+                if (lane == 31) at = atomicAdd(&s.list_at, in);
+                at = __shfl_sync(0xffffffffu, at, 31) + in - mine;
+                n += mine;
+#pragma unroll
+                for (int j = 0; j < 4 * kGroup; ++j)
+                    if (v[j] >= from) {
+                        if (at < kList) s.list[at] = key_of(v[j], first + i0 + j / 4 * 128 + j % 4);
+                        ++at;
+                    }
+            }
+            Sums a = {(u64)n, m, 0, 0};
             a.n = warp_sum64(a.n);
             a.m = warp_sum64(a.m);
             __syncthreads();
             if (lane == 0) { s.warp_sum[warp][0] = a.n; s.warp_sum[warp][1] = a.m; s.warp_sum[warp][2] = s.warp_sum[warp][3] = 0; }
+            const int was = turn;
             a = exchange();
             total = a.m;
-            return a.n > (u64)kList ? kList + 1 : (int)a.n;
+            if (a.n > (u64)kList) return kList + 1;
+            gather([&](int c) { return (int)s.sum[was][c][0]; });
+            return (int)a.n;
         };
         float from = least;
         int n_list = kList + 1;
@@ -488,11 +569,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             if (by_k && k == 1) {
                 from = mx;
             } else if (by_k && !all) {
-                for (int i = w0 + lane * 4; i < w1; i += 128) {
-                    const float4 v = load(i);
-                    const float top = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
+                auto count = [&](float top) {
                     float at;
                     if (may(top)) atomicAdd(&s.hist[bin_of(top, at)], 1u << p.off_shift);
+                };
+                if ((int64_t)k * 8 * kGroup <= p.V) {            // (half of the groups hold k ids, and hardly more than 1.4 k where they lie anyhow)
+                    for (int g = 0; g < n_groups; ++g) count(tops[g * 32]);
+                } else {
+                    for (int i = w0 + lane * 4; i < w1; i += 128) {
+                        const float4 v = load(i);
+                        count(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+                    }
                 }
                 read_bins(false);
                 from = below_bin(s.last_bin);
@@ -646,10 +733,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 u64 n0, m0, n_in, all = 0;
                 u64 lo = 0, hi = ~0ull;                          // (what is known of the key where the guess is off again and again)
                 bool far = false;
+                int was = 0;
                 for (int again = 0;; ++again) {
                     // what lies ahead of the bin, and the bin itself into the leader's list
-                    if (rank == 0 && tid == 0) s.list_at = 0;
-                    cluster.sync();
+                    if (tid == 0) s.list_at = 0;
+                    __syncthreads();
                     const bool rest = of_all && again == 0;
                     const Sums mine = warp_part([&](float l, int i, Sums& a) {
                         if (!may(l)) return;
@@ -663,8 +751,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         } else if (bin == b) {
                             a.n += 1ull << 32;
                             a.o += w;
-                            const int slot = atomicAdd(&lead->list_at, 1);
-                            if (slot < kList) lead->list[slot] = key_of(l, first + i);
+                            const int slot = atomicAdd(&s.list_at, 1);
+                            if (slot < kList) s.list[slot] = key_of(l, first + i);
                         } else {
                             a.t += w;
                         }
@@ -674,6 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         s.warp_sum[warp][0] = mine.n; s.warp_sum[warp][1] = mine.m; s.warp_sum[warp][2] = mine.o; s.warp_sum[warp][3] = mine.t;
                         s.warp_mass[warp] = mine.m;
                     }
+                    was = turn;
                     const Sums a = exchange();
                     n0 = a.n & 0xffffffffull;
                     n_in = a.n >> 32;
@@ -699,6 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     }
                     return lo;
                 }
+                gather([&](int c) { return (int)(s.sum[was][c][0] >> 32); });
                 if (rank == 0) {
                     const int n = (int)n_in;
                     // (the bin's range; the last bin is open, and goes by comparing)
