@@ -28,6 +28,8 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "mirror_internal.h"
 
 namespace cg = cooperative_groups;
@@ -40,6 +42,7 @@ constexpr int kMaxWarps = 16;                 // 512 threads a CTA, or 256
 constexpr int kBins = 2048;
 constexpr float kBinsPerNat = 64.f;
 constexpr int kList = 2048;                   // candidates that the leader ranks
+constexpr int kShort = 256;                   // so few that each is compared with each
 constexpr int kMaxCluster = 16;
 constexpr int kGroup = 4;                     // a group: this many of a thread's loads, 16 ids
 constexpr int kTable = 16;
@@ -86,7 +89,7 @@ struct alignas(16) Shared {
     u64 warp_sum[kMaxWarps][4];
     u64 warp_mass[kMaxWarps];                    // kept mass of the warps' parts
     u64 cut_key;                              // composite key of the last kept id
-    u64 kept;                                 // its front's mass
+    u64 kept, kept_mass;                      // ids of its front, their mass
     u64 base;
     int last_bin, list_at;                    // written by the leader
     int n_list, n_all;                        // ids up to last_bin, and in all bins
@@ -156,9 +159,9 @@ __device__ __forceinline__ u64 warp_incl64(u64 v) {
 }
 
 // A thread's w[], inclusive over the block: what lies before it, and all.
-template <int kPer>
+template <int kThreads, int kPer>
 __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& before) {
-    constexpr int kWarps = kList / kPer / 32;
+    constexpr int kWarps = kThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     u64 mine = 0;
 #pragma unroll
@@ -175,9 +178,9 @@ __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& 
 
 // list[0 .. n) in ascending order: sorted into bins over the logits from `hi` down, `scale` of them to a nat of it, and within a bin by
 // comparing all with all.
-template <int kThreads>
+template <int kThreads, int kPer>
 __device__ __noinline__ void sort_list(Shared& s, int n, float hi, float scale) {
-    constexpr int kPer = kList / kThreads;
+    constexpr int kBinsPer = kBins / kThreads;
     const int tid = threadIdx.x;
     auto place = [&](u64 key) { return (int)fminf(fmaxf((hi - logit_of(key)) * scale, 0.f), (float)(kBins - 1)); };
     __syncthreads();
@@ -191,13 +194,13 @@ __device__ __noinline__ void sort_list(Shared& s, int n, float hi, float scale) 
     }
     __syncthreads();
     {
-        u64 cnt[kPer], before;
+        u64 cnt[kBinsPer], before;
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) cnt[j] = s.hist[tid * kPer + j];
-        block_scan(s, cnt, before);
+        for (int j = 0; j < kBinsPer; ++j) cnt[j] = s.hist[tid * kBinsPer + j];
+        block_scan<kThreads>(s, cnt, before);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            s.hist[tid * kPer + j] = (uint32_t)before;
+        for (int j = 0; j < kBinsPer; ++j) {
+            s.hist[tid * kBinsPer + j] = (uint32_t)before;
             before += cnt[j];
         }
     }
@@ -214,6 +217,20 @@ __device__ __noinline__ void sort_list(Shared& s, int n, float hi, float scale) 
         for (int q = lo; q < end; ++q) ahead += s.ranked[q] < key[j];
         s.list[lo + ahead] = key[j];
     }
+    __syncthreads();
+}
+
+// The same for up to kShort of them: all with all.
+__device__ __forceinline__ void sort_short(Shared& s, int n) {
+    const int tid = threadIdx.x;
+    __syncthreads();
+    const u64 key = tid < n ? s.list[tid] : ~0ull;
+    int ahead = 0;
+    if (tid < n)
+#pragma unroll 4
+        for (int q = 0; q < n; ++q) ahead += s.list[q] < key;
+    __syncthreads();
+    if (tid < n) s.list[ahead] = key;
     __syncthreads();
 }
 
@@ -372,6 +389,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 
     u64 cut = ~0ull;                                             // composite key of the last id of the front
     int ahead_bin = -1;                                          // >= 0: the warps' masses ahead of that bin are in s.warp_mass
+    bool known = false;                                          // all of the front's are, and how many ids it has
+    u64 n_known = 0, m_known = 0;
     u64 Z = 0;
     if (!none && (by_k || by_p || by_m)) {
         const float parts = (float)(1 << p.off_bits);
@@ -625,89 +644,105 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 if (p.probs) fill(p.probs + (size_t)row * p.V, 0.f, p.vec_probs);
                 if (p.logits_out) fill(p.logits_out + (size_t)row * p.V, -INFINITY, p.vec_logits);
             }
-            if (rank == 0) {
-                sort_list<kThreads>(s, n_list, weigh.hi, weigh.hi - from > 0.f && !max_inf ? (float)(kBins - 1) / (weigh.hi - from) : 0.f);
-                u64 key[kPer];
-                u64 w[kPer], sel[kPer], before;
+            if (rank != 0) {
+                // (the rows are filled: the leader waits for those that are still there)
+                if (p.probs || p.logits_out) cluster.barrier_arrive();
+                return;
+            }
+            auto finish = [&](auto per) {
+                constexpr int P = decltype(per)::value;          // ids of a thread
+                if (P == 1) sort_short(s, n_list);
+                else sort_list<kThreads, P>(s, n_list, weigh.hi, weigh.hi - from > 0.f && !max_inf ? (float)(kBins - 1) / (weigh.hi - from) : 0.f);
+                u64 key[P], w[P], sel[P], before;
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const int r = tid * kPer + j;
+                for (int j = 0; j < P; ++j) {
+                    const int r = tid * P + j;
                     key[j] = r < n_list ? s.list[r] : ~0ull;
                     w[j] = r < n_list ? weigh(logit_of(key[j])) : 0ull;
                     sel[j] = by_k && r >= k ? 0ull : w[j];
                 }
-                const u64 part = block_scan(s, sel, before);
+                const u64 part = block_scan<kThreads>(s, sel, before);
                 const double want = top_p * (double)(whole_total ? total : part);
                 int kept = 0;
                 u64 kept_mass = 0;
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const int r = tid * kPer + j;
+                for (int j = 0; j < P; ++j) {
+                    const int r = tid * P + j;
                     const bool stays = r < n_list && (r == 0 || ((!by_k || r < k) && (!by_p || (double)before < want) && (!by_m || w[j] >= min_w)));
                     kept += stays;
-                    if (stays) kept_mass += w[j];
+                    if (stays) {
+                        kept_mass += w[j];
+                        if (P == 1) s.drawn[tid] = {w[j], (uint32_t)key[j], 0u};
+                    }
                     before += sel[j];
                 }
                 kept = __reduce_add_sync(0xffffffffu, kept);
                 kept_mass = warp_sum64(kept_mass);
                 if (lane == 0) { s.warp_sum[warp][2] = (u64)kept; s.warp_sum[warp][3] = kept_mass; }
+                if (P > 1) {
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) s.ranked[tid * kPer + j] = 0;         // (from here on: masses of buckets of ids)
-                if (tid == 0) s.list_at = 0;
+                    for (int j = 0; j < kPer; ++j) s.ranked[tid * kPer + j] = 0;     // (from here on: masses of buckets of ids)
+                    if (tid == 0) s.list_at = 0;
+                }
                 __syncthreads();
                 int n = 0;
                 Z = 0;
 #pragma unroll
                 for (int q = 0; q < kWarps; ++q) { n += (int)s.warp_sum[q][2]; Z += s.warp_sum[q][3]; }
-                // the draw: the bucket of ids in which the sum over ids passes the uniform's share, then the id within it
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (tid * kPer + j < n) atomicAdd(&s.ranked[(uint32_t)key[j] >> p.id_shift], w[j]);
-                __syncthreads();
-                u64 bucket[kPer];
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) bucket[j] = s.ranked[tid * kPer + j];
-                block_scan(s, bucket, before);
                 const double t = fmax((double)p.u[row], 0.0) * (double)Z;
                 const u64 target = t >= (double)Z ? Z - 1 : (u64)t;                 // the first id whose inclusive sum is above it
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    if (before <= target && before + bucket[j] > target) {
-                        s.bucket = tid * kPer + j;
-                        s.base = before;
-                    }
-                    before += bucket[j];
-                }
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (tid * kPer + j < n && (int)((uint32_t)key[j] >> p.id_shift) == s.bucket) s.drawn[atomicAdd(&s.list_at, 1)] = {w[j], (uint32_t)key[j], 0u};
-                __syncthreads();
-                for (int q = tid; q < s.list_at; q += kThreads) {
-                    const Drawn d = s.drawn[q];
-                    u64 sum = s.base;
-                    for (int q2 = 0; q2 < s.list_at; ++q2)
-                        if (s.drawn[q2].id < d.id) sum += s.drawn[q2].w;
+                // the draw: of few, each adds up those of the lower ids; of many the bucket of ids in which the sum over ids passes the target, then
+                // the id within it
+                auto draw = [&](const Drawn& d, u64 sum, int of) {
+                    for (int q = 0; q < of; ++q)
+                        if (s.drawn[q].id < d.id) sum += s.drawn[q].w;
                     if (sum <= target && sum + d.w > target) {
                         p.token[row] = (int32_t)d.id;
                         if (p.logprob) p.logprob[row] = (float)log((double)d.w / (double)Z);
                         if (p.n_kept) p.n_kept[row] = n;
                     }
+                };
+                if (P == 1) {
+                    if (tid < n) draw({w[0], (uint32_t)key[0], 0u}, 0, n);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < P; ++j)
+                        if (tid * P + j < n) atomicAdd(&s.ranked[(uint32_t)key[j] >> p.id_shift], w[j]);
+                    __syncthreads();
+                    u64 bucket[kPer];
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) bucket[j] = s.ranked[tid * kPer + j];
+                    block_scan<kThreads>(s, bucket, before);
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        if (before <= target && before + bucket[j] > target) {
+                            s.bucket = tid * kPer + j;
+                            s.base = before;
+                        }
+                        before += bucket[j];
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int j = 0; j < P; ++j)
+                        if (tid * P + j < n && (int)((uint32_t)key[j] >> p.id_shift) == s.bucket) s.drawn[atomicAdd(&s.list_at, 1)] = {w[j], (uint32_t)key[j], 0u};
+                    __syncthreads();
+                    for (int q = tid; q < s.list_at; q += kThreads) draw(s.drawn[q], s.base, s.list_at);
                 }
                 if (!p.probs && !p.logits_out) return;
                 cluster.sync();                                  // (the rows are filled)
                 const double unit = (double)Z * p.two_ms, inv = 1.0 / unit, ln_z = log(unit);
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    if (tid * kPer + j >= n) break;
+                for (int j = 0; j < P; ++j) {
+                    if (tid * P + j >= n) break;
                     const float l = logit_of(key[j]);
                     const size_t at = (size_t)row * p.V + (uint32_t)key[j];
                     if (p.probs) p.probs[at] = (float)(weigh.exact(l) * inv);
                     if (p.logits_out) p.logits_out[at] = (float)((max_inf ? 0.0 : ((double)l - weigh.max) * c) * ln2T - ln_z * (double)p.temperature);
                 }
-                return;
-            }
-            if (p.probs || p.logits_out) cluster.sync();
+            };
+            if (n_list <= kShort) finish(std::integral_constant<int, 1>());
+            else if (n_list <= kList / 2) finish(std::integral_constant<int, kPer / 2>());
+            else finish(std::integral_constant<int, kPer>());
             return;
         }
         {
@@ -729,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             };
             // The smallest key whose front (count, mass, and the mass of all ids where that is asked for) fulfils `done`, which is monotone;
             // guessed to lie in bin `b`.
-            auto end_of = [&](int b, bool by_mass, bool of_all, auto done) -> u64 {
+            auto end_of = [&](int b, bool of_all, auto done) -> u64 {
                 u64 n0, m0, n_in, all = 0;
                 u64 lo = 0, hi = ~0ull;                          // (what is known of the key where the guess is off again and again)
                 bool far = false;
@@ -744,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         float at;
                         const int bin = bin_of(l, at);
                         if (bin > b && !rest) return;
-                        const u64 w = by_mass ? weigh(l) : 0ull;
+                        const u64 w = weigh(l);
                         if (bin < b) {
                             ++a.n;
                             a.m += w;
@@ -768,7 +803,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     n_in = a.n >> 32;
                     m0 = a.m;
                     if (rest) all = a.m + a.o + a.t;
-                    ahead_bin = by_mass ? b : -1;
+                    ahead_bin = b;
+                    known = false;
                     const bool early = n0 > 0 && done(n0, m0, all), late = b < kBins - 1 && !done(n0 + n_in, m0 + a.o, all);
                     far = (early || late) && again >= 3;
                     // (the bin's own keys, or all ahead of it, or all behind it)
@@ -792,16 +828,16 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 if (rank == 0) {
                     const int n = (int)n_in;
                     // (the bin's range; the last bin is open, and goes by comparing)
-                    sort_list<kThreads>(s, n, weigh.hi - (float)b * T * (1.f / kBinsPerNat), max_inf || b == kBins - 1 ? 0.f : (float)(kBins - 1) * kBinsPerNat * inv_T);
+                    sort_list<kThreads, kPer>(s, n, weigh.hi - (float)b * T * (1.f / kBinsPerNat), max_inf || b == kBins - 1 ? 0.f : (float)(kBins - 1) * kBinsPerNat * inv_T);
                     if (tid == 0) s.list_at = n - 1;
-                    u64 w[kPer], at;
+                    u64 w[kPer], before;
 #pragma unroll
                     for (int j = 0; j < kPer; ++j) {
                         const int r = tid * kPer + j;
-                        w[j] = by_mass && r < n ? weigh(logit_of(s.list[r])) : 0ull;
+                        w[j] = r < n ? weigh(logit_of(s.list[r])) : 0ull;
                     }
-                    block_scan(s, w, at);
-                    at += m0;
+                    block_scan<kThreads>(s, w, before);
+                    u64 at = before + m0;
 #pragma unroll
                     for (int j = 0; j < kPer; ++j) {
                         const int r = tid * kPer + j;
@@ -809,21 +845,40 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         if (r < n && done(n0 + r + 1, at, all)) { atomicMin(&s.list_at, r); break; }
                     }
                     __syncthreads();
-                    if (tid < C) cluster.map_shared_rank(&s, tid)->cut_key = s.list[s.list_at];
+                    if (tid < C) {
+                        Shared* const o = cluster.map_shared_rank(&s, tid);
+                        o->cut_key = s.list[s.list_at];
+                        o->kept = n0 + s.list_at + 1;
+                    }
+                    // (what stays of the bin belongs to warps' parts, too)
+                    at = before + m0;
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        const int r = tid * kPer + j;
+                        if (r > s.list_at) break;
+                        at += w[j];
+                        if (r == s.list_at)
+                            for (int c = 0; c < C; ++c) cluster.map_shared_rank(&s, c)->kept_mass = at;
+                        const int id = (int)(uint32_t)s.list[r], of = id / p.part;
+                        atomicAdd(&cluster.map_shared_rank(&s, of)->warp_mass[(id - of * p.part) / per_warp], w[j]);
+                    }
                 }
+                known = true;
                 cluster.sync();
                 const u64 c = s.cut_key;
+                n_known = s.kept;
+                m_known = s.kept_mass;
                 cluster.sync();                                  // (the next one may be written)
                 return c;
             };
             total = 0;
             const bool cuts_k = by_k && k < s.n_all;             // (there may be fewer that may be kept)
             if (cuts_k) {
-                cut = end_of(s.bin_k, false, false, [&](u64 n, u64, u64) { return n >= (u64)k; });
-                if (by_p) total = front(cut).m;
+                cut = end_of(s.bin_k, false, [&](u64 n, u64, u64) { return n >= (u64)k; });
+                if (by_p) total = known ? m_known : front(cut).m;
             }
             if (by_p) {
-                const u64 c = end_of(s.bin_p, true, !cuts_k, [&](u64 n, u64 m, u64 all) { return n >= 1 && (double)m >= top_p * (double)(cuts_k ? total : all); });
+                const u64 c = end_of(s.bin_p, !cuts_k, [&](u64 n, u64 m, u64 all) { return n >= 1 && (double)m >= top_p * (double)(cuts_k ? total : all); });
                 cut = min(cut, c);
             }
             if (by_m) {
@@ -839,7 +894,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     if (lane == 0) s.base = ((u64)~hi << 32) | 0xffffffffull;
                 }
                 __syncthreads();
-                if (s.base < cut) { cut = s.base; ahead_bin = -1; }
+                if (s.base < cut) { cut = s.base; ahead_bin = -1; known = false; }
             }
         }
     }
@@ -849,13 +904,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     auto kept = [&](float l, int i) { return l > cut_l || (l == cut_l && i <= cut_i); };
     {
         // (ahead of the bin in which the front ends the masses are known)
-        const Sums mine = warp_part([&](float l, int i, Sums& a) {
-            if (!kept(l, i)) return;
-            ++a.n;
-            float at;
-            if (ahead_bin < 0 || bin_of(l, at) >= ahead_bin) a.m += weigh(l);
-        });
-        const u64 mass = mine.m + (ahead_bin < 0 ? 0ull : s.warp_mass[warp]);
+        Sums mine = {rank == 0 && warp == 0 ? n_known : 0ull, 0, 0, 0};
+        if (!known)
+            mine = warp_part([&](float l, int i, Sums& a) {
+                if (!kept(l, i)) return;
+                ++a.n;
+                float at;
+                if (ahead_bin < 0 || bin_of(l, at) >= ahead_bin) a.m += weigh(l);
+            });
+        const u64 mass = mine.m + (known || ahead_bin >= 0 ? s.warp_mass[warp] : 0ull);
         __syncthreads();
         if (lane == 0) {
             s.warp_sum[warp][0] = mine.n; s.warp_sum[warp][1] = mass; s.warp_sum[warp][2] = s.warp_sum[warp][3] = 0;
