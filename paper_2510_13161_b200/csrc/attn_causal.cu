@@ -78,13 +78,14 @@ __device__ Begin range_begin(const CausalParams& p, const Sums& s, long long tot
     }
     u.b = lo;
     const int T = s.slots[lo + 1] - s.slots[lo], per = T + kUnitSlots;
-    const int in = (int)(rem - (long long)p.Hkv * s.cost(lo));
-    u.h = in / per;
-    u.t = max(0, in - u.h * per - kUnitSlots);
+    const long long in = rem - (long long)p.Hkv * s.cost(lo);
+    u.h = (int)(in / per);
+    const int in_unit = (int)(in - (long long)u.h * per);
+    u.t = max(0, in_unit - kUnitSlots);
     const int tol = (int)min(8ll, total / ctas >> 2);
     if (!never_cut && u.t <= tol) u.t = 0;
     // (never cut: the unit belongs to the CTA that has its larger part)
-    if (u.t > 0 && (never_cut ? 2 * (in - u.h * per) > per : T - u.t <= tol)) u.t = T;
+    if (u.t > 0 && (never_cut ? 2ll * in_unit > per : T - u.t <= tol)) u.t = T;
     if (never_cut && u.t < T) u.t = 0;
     u.x = u.layer * per_layer + (long long)p.Hkv * s.slots[lo] + (long long)u.h * T + u.t;
     if (u.t == T) {
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<D, kWarps>::kCtas) attn_token
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float mw = s_ml[(w * kRows + row) * 2];
-                if (mw != -INFINITY) Ls = fmaf(exp2f(mw - M), s_ml[(w * kRows + row) * 2 + 1], Ls);
+                Ls = fmaf(mw == -INFINITY ? 0.f : exp2f(mw - M), s_ml[(w * kRows + row) * 2 + 1], Ls);     // (0 times a sum that is no number is none)
             }
             float4 acc = *reinterpret_cast<const float4*>(s_o + row * C::kPitch + col);
 #pragma unroll
@@ -500,14 +501,13 @@ __global__ void __launch_bounds__(kMergeThreads) attn_token_merge_kernel(const _
             float top = M;
 #pragma unroll
             for (int k = 0; k < kMergeBatch; ++k) top = fmaxf(top, m[k]);
-            if (top == -INFINITY) continue;
-            const float keep = exp2f(M - top);
+            const float keep = M == -INFINITY ? 0.f : exp2f(M - top);
             M = top;
             L *= keep;
             acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
 #pragma unroll
             for (int k = 0; k < kMergeBatch; ++k) {
-                const float f = exp2f(m[k] - top);                  // (a part that saw nothing: 0)
+                const float f = m[k] == -INFINITY ? 0.f : exp2f(m[k] - top);         // (a part that saw nothing)
                 L = fmaf(f, l[k], L);
                 acc.x = fmaf(f, v[k].x, acc.x); acc.y = fmaf(f, v[k].y, acc.y); acc.z = fmaf(f, v[k].z, acc.z); acc.w = fmaf(f, v[k].w, acc.w);
             }

@@ -88,7 +88,6 @@ __device__ __forceinline__ Keys pair_keys(const PromptParams& p, int n, int pref
 }
 
 // ---- a CTA's way through its units -----------------------------------------------------------------------------
-struct Ctrl;
 struct Segment {
     Unit u;
     int t_first, t_last;                  // tiles [t_first, t_last) of the unit

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
             if (b >= 0) {
                 const long long at = (long long)p.prefix_len[b] + (row - first);
                 if (at >= 0 && at < (long long)p.max_pages * 16) {
-                    const int page = p.page_table[(size_t)b * p.max_pages + (int)at / 16];
+                    const int page = p.page_table[(size_t)b * p.max_pages + (size_t)(at / 16)];
                     if (page >= 0 && page < p.num_pages) slot = ((long long)page * p.Hkv * 16 + at % 16) * p.d;
                 }
                 if (slot < 0) report(p.status, 820);

@@ -146,6 +146,36 @@ def test_masked_infinite_and_missing_logits():
         check(x, T=0.8, k=k, p=p, mp=mp, seed=11)
 
 
+@pytest.mark.parametrize("M", [3, 40])
+@pytest.mark.parametrize("k", [1, 2, 255, 256, 257, 800, 1023, 1024, 1025, 1399, 1400, 1401, 1600, 2047, 2048, 2049])
+def test_fronts_of_every_length_of_list(M, k):
+    """Few candidates are compared each with each, more are sorted, and fronts that are longer than the list are found by their end."""
+    x = logits_of(M, 40961, k, std=1.5, leaders=0)
+    check(x, k=k, seed=k)
+    check(x[:3], T=1.2, k=k, p=[0.9, 0.3, 1.0], mp=[0.0, 0.0, 0.04], seed=k + 1)
+
+
+@pytest.mark.parametrize("V", [257, 2048, 2049])
+def test_rows_as_long_as_the_list(V):
+    check(logits_of(4, V, V, std=0.5, leaders=0), k=[0, 300, 0, 256], p=[0.9, 1.0, 0.99, 0.8], mp=[0.0, 0.0, 0.3, 0.05], seed=V)
+
+
+@pytest.mark.parametrize("M", [2, 40])
+def test_leaders_that_lie_together(M):
+    """The largest logits side by side, in order, or in one thread's reach: the candidates of few groups are many."""
+    x = logits_of(M, 60000, 77, leaders=0)
+    x[0, 1000:6000] += 30
+    x[1] = np.sort(x[1])
+    if M > 2:
+        x[2] = np.sort(x[2])[::-1]
+        x[3, 128 * np.arange(16)] += 30
+        x[4, 59990:] += 30
+        x[5, :3000] = 9.0
+    for k, p, mp in ((50, None, None), (1000, 0.9, None), (None, None, 0.2), (None, 0.6, 0.3), (1, None, None)):
+        check(x[:6], T=0.9, k=k, p=p, mp=mp, seed=M)
+    check(x, k=200, seed=M + 1)
+
+
 def test_uniforms_at_their_ends_and_greedy_rows():
     x = logits_of(6, 2000, 6)
     check(x, u=[0.0, np.nextafter(np.float32(1), np.float32(0)), 0.5, 1e-30, 0.25, 0.75], p=0.9)
