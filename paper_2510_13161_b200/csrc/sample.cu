@@ -45,7 +45,7 @@ constexpr int kList = 2048;                   // candidates that the leader rank
 constexpr int kShort = 256;                   // so few that each is compared with each
 constexpr int kMaxCluster = 16;
 constexpr int kGroup = 4;                     // a group: this many of a thread's loads, 16 ids
-constexpr int kTable = 16;
+constexpr int kTable = 64;
 constexpr int kQuickK = 1400;                 // (the largest of every four: hardly more than k candidates then)
 constexpr int kMaxPart = 40960;               // ids of a CTA
 static_assert(kMaxPart / (4 * kGroup) <= 2 * kList && kMaxPart % (1024 * kGroup) == 0, "a part's groups have their place");
@@ -71,7 +71,7 @@ struct SampleParams {
     float* probs;
     float* logits_out;
     double two_s, two_ms;                     // 2^S, 2^-S
-    double table[kTable];                     // 2^(j / 16)
+    double table[kTable];                     // 2^(j / 64)
 };
 
 struct Sums {
@@ -96,7 +96,8 @@ struct alignas(16) Shared {
     int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
     int bucket;
     float row_mass;
-    alignas(16) double table[kTable];         // 2^(j / 16)
+    alignas(16) double table[kTable];         // 2^(j / 64)
+    double shares[kTable];                    // the same over the kept mass
     union alignas(16) {
         uint32_t hist[kBins];                 // counts and offsets; the leader's: then where each bin's candidates go
         Drawn drawn[kBins / 4];               // (the candidates that the draw has to look at one by one)
@@ -112,35 +113,35 @@ static_assert(sizeof(Shared) % 16 == 0, "the logits behind it are read 16 bytes 
 __device__ __forceinline__ float unkey(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ float logit_of(u64 key) { return unkey(~(uint32_t)(key >> 32)); }
 
-// round(2^S exp((l - max) / T)): y = (l - max) log2(e) / T = n / 16 + f with |f| <= 1/32; 2^(n / 16) from a table of sixteenths (16
-// doubles fill the 32 banks once, so any lanes may read any of them), 2^f by its Taylor series to f^6 (the next term is below 5e-16).
+// round(2^S exp((l - max) / T)): y = (l - max) log2(e) / T = n / 64 + f with |f| <= 1/128; 2^(n / 64) from a table, 2^f by its Taylor series to
+// f^4 (the next term is below 4e-14), or to f^3 (4e-11) where the result is rounded to fp32.  (Against a table of sixteenths and f^6 the
+// table's bank conflicts cost less than the operations, of which double precision has 64 a cycle and SM.)
 struct Weigh {
     double max, c;                            // c: log2(e) / T, as far as weights can tell (the next number below the maximum at 2^-900)
     float lo, hi;                             // l is taken between them: 2^-900 is nothing, and a maximum of +inf counts as a number (c = 0)
     int shift;
     const double* table;
     __device__ __forceinline__ double y_of(float l) const { return ((double)fminf(fmaxf(l, lo), hi) - max) * c; }
-    __device__ __forceinline__ double exp2_scaled(double y, int s) const {      // 2^(y + s)
-        const double magic = 422212465065984.0;                  // 1.5 * 2^48: the sum's low bits are the nearest sixteenth
+    template <int kDegree>
+    __device__ __forceinline__ double exp2_scaled(double y, int s, const double* of) const {      // of[0] 2^(y + s)
+        const double magic = 105553116266496.0;                  // 1.5 * 2^46: the sum's low bits are the nearest 64th
         const double t = y + magic;
         const int n = __double2loint(t);
         const double f = y - (t - magic);
-        double r = 1.54035303933816061e-04;                        // ln(2)^k / k!, k = 6 .. 0
-        r = fma(r, f, 1.33335581464284411e-03);
-        r = fma(r, f, 9.61812910762847688e-03);
-        r = fma(r, f, 5.55041086648215762e-02);
+        double r = 5.55041086648215762e-02;                        // ln(2)^k / k!, k = 4 or 3 .. 0
+        if (kDegree == 4) r = fma(9.61812910762847688e-03, f, r);
         r = fma(r, f, 2.40226506959100694e-01);
         r = fma(r, f, 6.93147180559945286e-01);
         r = fma(r, f, 1.0);
-        r *= table[n & (kTable - 1)];
-        return __hiloint2double(__double2hiint(r) + (((n >> 4) + s) << 20), __double2loint(r));
+        r *= of[n & (kTable - 1)];
+        return __hiloint2double(__double2hiint(r) + (((n >> 6) + s) << 20), __double2loint(r));
     }
     // (of an id that may be kept)
     __device__ __forceinline__ u64 operator()(float l) const {
-        const double w = exp2_scaled(y_of(l), shift);
+        const double w = exp2_scaled<4>(y_of(l), shift, table);
         return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;          // + 2^52: the low bits are the integer
     }
-    __device__ __forceinline__ double exact(float l) const { return exp2_scaled(y_of(l), 0); }
+    __device__ __forceinline__ double share(float l, const double* shares) const { return exp2_scaled<3>(y_of(l), 0, shares); }
 };
 
 __device__ __forceinline__ u64 warp_sum64(u64 v) {
@@ -730,13 +731,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 }
                 if (!p.probs && !p.logits_out) return;
                 cluster.sync();                                  // (the rows are filled)
-                const double unit = (double)Z * p.two_ms, inv = 1.0 / unit, ln_z = log(unit);
+                const double unit = (double)Z * p.two_ms, ln_z = log(unit);
+                if (tid < kTable) s.shares[tid] = s.table[tid] / unit;
+                __syncthreads();
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
                     if (tid * P + j >= n) break;
                     const float l = logit_of(key[j]);
                     const size_t at = (size_t)row * p.V + (uint32_t)key[j];
-                    if (p.probs) p.probs[at] = (float)(weigh.exact(l) * inv);
+                    if (p.probs) p.probs[at] = (float)weigh.share(l, s.shares);
                     if (p.logits_out) p.logits_out[at] = (float)((max_inf ? 0.0 : ((double)l - weigh.max) * c) * ln2T - ln_z * (double)p.temperature);
                 }
             };
@@ -774,24 +777,32 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     if (tid == 0) s.list_at = 0;
                     __syncthreads();
                     const bool rest = of_all && again == 0;
-                    const Sums mine = warp_part([&](float l, int i, Sums& a) {
-                        if (!may(l)) return;
+                    uint32_t n_ahead = 0, n_bin = 0;
+                    u64 m_ahead = 0, m_bin = 0, m_all = 0;
+                    for (int i = w0 + lane * 4; i < w1; i += 128) {
+                        const float4 v4 = load(i);
+                        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+                        int bin[4];
                         float at;
-                        const int bin = bin_of(l, at);
-                        if (bin > b && !rest) return;
-                        const u64 w = weigh(l);
-                        if (bin < b) {
-                            ++a.n;
-                            a.m += w;
-                        } else if (bin == b) {
-                            a.n += 1ull << 32;
-                            a.o += w;
-                            const int slot = atomicAdd(&s.list_at, 1);
-                            if (slot < kList) s.list[slot] = key_of(l, first + i);
-                        } else {
-                            a.t += w;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) bin[j] = may(v[j]) ? bin_of(v[j], at) : kBins;
+                        const int least_bin = min(min(bin[0], bin[1]), min(bin[2], bin[3]));
+                        if (least_bin > (rest ? kBins - 1 : b)) continue;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const u64 any = weigh(v[j]), w = bin[j] < kBins ? any : 0ull;
+                            m_all += w;
+                            m_ahead += bin[j] < b ? w : 0ull;
+                            n_ahead += bin[j] < b;
+                            if (bin[j] == b) {
+                                ++n_bin;
+                                m_bin += w;
+                                const int slot = atomicAdd(&s.list_at, 1);
+                                if (slot < kList) s.list[slot] = key_of(v[j], first + i + j);
+                            }
                         }
-                    });
+                    }
+                    const Sums mine = {warp_sum64(((u64)n_bin << 32) | n_ahead), warp_sum64(m_ahead), warp_sum64(m_bin), warp_sum64(m_all)};
                     __syncthreads();
                     if (lane == 0) {
                         s.warp_sum[warp][0] = mine.n; s.warp_sum[warp][1] = mine.m; s.warp_sum[warp][2] = mine.o; s.warp_sum[warp][3] = mine.t;
@@ -802,7 +813,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     n0 = a.n & 0xffffffffull;
                     n_in = a.n >> 32;
                     m0 = a.m;
-                    if (rest) all = a.m + a.o + a.t;
+                    if (rest) all = a.t;
                     ahead_bin = b;
                     known = false;
                     const bool early = n0 > 0 && done(n0, m0, all), late = b < kBins - 1 && !done(n0 + n_in, m0 + a.o, all);
@@ -967,7 +978,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         }
     }
     if (p.probs || p.logits_out) {
-        const double unit = (double)Z * p.two_ms, inv = 1.0 / unit, ln_z = log(unit);
+        const double unit = (double)Z * p.two_ms, ln_z = log(unit);
+        if (tid < kTable) s.shares[tid] = s.table[tid] / unit;   // (nothing kept: not read)
+        __syncthreads();
         float* const probs = p.probs ? p.probs + (size_t)row * p.V + first : nullptr;
         float* const lg = p.logits_out ? p.logits_out + (size_t)row * p.V + first : nullptr;
         for (int i = w0 + lane * 4; i < w1; i += 128) {
@@ -977,7 +990,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bool in_front = kept(v[j], i + j);
-                a[j] = in_front && probs ? (float)(weigh.exact(v[j]) * inv) : 0.f;
+                a[j] = in_front && probs ? (float)weigh.share(v[j], s.shares) : 0.f;
                 b[j] = in_front && lg ? (float)((max_inf ? 0.0 : ((double)v[j] - weigh.max) * c) * ln2T - ln_z * (double)p.temperature) : -INFINITY;
             }
             const bool whole = i + 4 <= n_mine;
