@@ -745,6 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             };
             if (n_list <= kShort) finish(std::integral_constant<int, 1>());
             else if (n_list <= kList / 2) finish(std::integral_constant<int, kPer / 2>());
+            else if (n_list <= kList / 4 * 3) finish(std::integral_constant<int, kPer / 4 * 3>());
             else finish(std::integral_constant<int, kPer>());
             return;
         }
