@@ -12,8 +12,8 @@
 // more of a row, get more rows through than two large ones (520 rows x 128256 ids: 435 us against 541 when this was changed).
 //   1  load, maximum over the cluster (the logits leave HBM once)
 //   2  (rows of up to kList ids go to 4 as they are, Top-k of one asks for the maximum alone)
-//      Top-k of up to kQuickK: a histogram of the largest logits of groups of 16 (or of every four, where groups are few) says down to which logit at least k ids lie; Min-p says
-//      so by itself.  Top-p of the whole row: a histogram of z in 2048 bins of 1/64, how many ids each holds and where in the bin they lie on
+//      Top-k of up to kQuickK: a histogram of the largest logits of groups of 16 (or of every four, where groups are few) says down to which
+//      logit at least k ids lie; Min-p says so by itself.  Top-p of the whole row: a histogram of z in 2048 bins of 1/64, how many ids each holds and where in the bin they lie on
 //      average, packed in one word, which gives a bin's mass to 10^-3
 //   3  the leading CTA adds the histograms up and reads off the bin in which each filter's front ends, Top-p's by estimate
 //   4  if at most kList ids lie ahead of a logit that surely lies behind the end of the front, they go to the leader, which ranks them and
@@ -21,10 +21,10 @@
 //   4' otherwise only the bin in which the front ends goes to the leader; what lies ahead of it is counted and summed by all.  (A bin
 //      of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
 //   5  the drawn token, by the warps' masses, and the filtered distribution
-// What bounds it: double-precision arithmetic (18 operations an id, 64 a cycle and SM) where Top-p or a draw takes the whole row, the
+// What bounds it: double-precision arithmetic (14 operations an id, 64 a cycle and SM) where Top-p or a draw takes the whole row, the
 // bytes otherwise; for a row alone the cluster's barriers and code that runs once.  Measured on a B200: one row of 152064 ids under all
-// three filters 16.7 us (0.1 us of bytes); 64 rows x 128256 under Top-p 0.9, probabilities written, 109 us; 520 rows x 128256 under Top-k 1000
-// and Top-p 0.98, logits written, 289 us (1.85 TB/s).
+// three filters 14.8 us (0.1 us of bytes); 64 rows x 128256 under Top-p 0.9, probabilities written, 93 us; 520 rows x 128256 under Top-k 1000
+// and Top-p 0.98, logits written, 179 us (3.0 TB/s).
 #include <cooperative_groups.h>
 #include <math.h>
 
