@@ -62,9 +62,10 @@ struct Begin {
 // Slots of a head's units, and how many units have any, summed over the requests.
 struct Sums {
     const int *slots, *units;             // [B + 1] each
-    __device__ __forceinline__ int cost(int b) const { return slots[b] + kUnitSlots * units[b]; }
+    int of_slot, of_unit;                 // what a slot and a unit cost
+    __device__ __forceinline__ int cost(int b) const { return of_slot * slots[b] + of_unit * units[b]; }
 };
-// Where CTA c's range begins.  The sequence is split evenly by cost, kUnitSlots for a unit and one for each of its slots.  never_cut: a range
+// Where CTA c's range begins.  The sequence is split evenly by cost.  never_cut: a range
 // begins with a unit; else a boundary close to a unit's is moved there (a cut costs a record and a merge).
 __device__ Begin range_begin(const CausalParams& p, const Sums& s, long long total, int ctas, int c, bool never_cut) {
     const long long per_layer = (long long)p.Hkv * s.slots[p.B];
@@ -79,11 +80,11 @@ __device__ Begin range_begin(const CausalParams& p, const Sums& s, long long tot
         if ((long long)p.Hkv * s.cost(mid + 1) > rem) hi = mid; else lo = mid + 1;
     }
     u.b = lo;
-    const int T = s.slots[lo + 1] - s.slots[lo], per = T + kUnitSlots;
+    const int T = s.slots[lo + 1] - s.slots[lo], per = s.of_slot * T + s.of_unit;
     const long long in = rem - (long long)p.Hkv * s.cost(lo);
     u.h = (int)(in / per);
     const int in_unit = (int)(in - (long long)u.h * per);
-    u.t = max(0, in_unit - kUnitSlots);
+    u.t = max(0, in_unit - s.of_unit);
     const int tol = (int)min(8ll, total / ctas >> 2);
     if (!never_cut && u.t <= tol) u.t = 0;
     // (never cut: the unit belongs to the CTA that has its larger part)
@@ -166,8 +167,12 @@ __global__ void __launch_bounds__(32 * kWarps, Cfg<D, kWarps>::kCtas) attn_token
             acc += __shfl_sync(0xffffffffu, sum, 31);
         }
         __syncwarp();
-        const Sums sums = {cum, cum_units};
-        const long long lh = (long long)p.L * p.Hkv, total = lh * (acc + kUnitSlots * units), most = max(lh * units, lh * acc / kMinShare);
+        // kUnitSlots for a unit and one for each of its slots; whole units that are no more than the CTAs get one each, whatever their
+        // lengths (by cost the shorter ones shared: 159 units of 1 to 3 slots 17.0 -> 10.2 us)
+        const long long lh = (long long)p.L * p.Hkv;
+        const bool one_each = never_cut && lh * units <= (long long)gridDim.x;
+        const Sums sums = {cum, cum_units, one_each ? 0 : 1, one_each ? 1 : kUnitSlots};
+        const long long total = lh * sums.cost(p.B), most = one_each ? lh * units : max(lh * units, lh * acc / kMinShare);
         const int ctas = (int)min((long long)gridDim.x, max(most, 1ll));
         if (lane < 2) {
             s_begin[lane] = range_begin(p, sums, total, ctas, (int)blockIdx.x + lane, never_cut != 0);
