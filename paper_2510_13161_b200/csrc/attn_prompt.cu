@@ -114,15 +114,17 @@ __device__ __forceinline__ StreamRows stream_rows(const PromptParams& p, const S
     const int t0 = s.u.tok + g * p.nt, t1 = min(t0 + p.nt, s.u.n) - 1;
     return {s.u.prefix + t0, s.u.prefix + t1};
 }
-__device__ __forceinline__ bool tile_seen(const PromptParams& p, const Segment& s, const StreamRows& r, int t) {
-    const int key0 = s.keys.page(t * kTileSlots) * kSlotTok, key1 = s.keys.page(min(t * kTileSlots + kTileSlots, s.keys.slots) - 1) * kSlotTok + kSlotTok - 1;
+// (Segments go to a function out of line by their address, so what is read of them again comes from local memory: Keys and StreamRows are
+// passed as values, which stay in registers.)
+__device__ __forceinline__ bool tile_seen(const PromptParams& p, Keys k, StreamRows r, int t) {
+    const int key0 = k.page(t * kTileSlots) * kSlotTok, key1 = k.page(min(t * kTileSlots + kTileSlots, k.slots) - 1) * kSlotTok + kSlotTok - 1;
     return r.last >= r.first && key0 <= r.last && (p.c.window == 0 || key1 > r.first - p.c.window || key0 < p.c.n_sink);
 }
 
 // ... and of how many of the tile's slots, from its first?  (What lies behind the stream's last row is not multiplied.)
-__device__ __forceinline__ int slots_seen(const Segment& s, const StreamRows& r, int t) {
-    const int most = min(kTileSlots, s.keys.slots - t * kTileSlots), page0 = s.keys.page(t * kTileSlots);
-    const int jump = s.keys.sink_slots > t * kTileSlots ? s.keys.from - s.keys.sink_slots : 0;         // (sinks and window in one tile: by its last slot)
+__device__ __forceinline__ int slots_seen(Keys k, StreamRows r, int t) {
+    const int most = min(kTileSlots, k.slots - t * kTileSlots), page0 = k.page(t * kTileSlots);
+    const int jump = k.sink_slots > t * kTileSlots ? k.from - k.sink_slots : 0;         // (sinks and window in one tile: by its last slot)
     return max(1, min(most, r.last / kSlotTok + 1 - page0 + (jump > 0 ? most : 0)));
 }
 
@@ -387,15 +389,15 @@ struct Cfg {
 // Scores of tokens that the row at position `pos` does not see become -inf, in TMEM; `rows` are the stream's positions.  A slot at a time,
 // and little code: most of a tile's slots are seen by all rows, or by none, and what runs once per unit is bound by the fetch of its
 // instructions (32 columns at a time, unrolled, with the maximum taken on the way: 4400 cycles, this and tile_max 2500).
-__device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, int slots, const Keys& k, int pos, const StreamRows& rows, int window, int n_sink) {
-    const int first_lo = window > 0 ? rows.first - window : -1, last_lo = window > 0 ? rows.last - window : -1;     // (what lies up to there is out of the window)
+__device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, int slots, int sink_slots, int from, int n_slots, int pos, int row_first, int row_last, int window, int n_sink) {
+    const int first_lo = window > 0 ? row_first - window : -1, last_lo = window > 0 ? row_last - window : -1;     // (what lies up to there is out of the window)
 #pragma unroll 1
     for (int c = 0; c < slots; ++c, s_addr += 16) {
-        const int key0 = k.page(min(slot0 + c, k.slots - 1)) * kSlotTok, key1 = key0 + kSlotTok - 1;
-        const bool there = slot0 + c < k.slots;
-        if (there && key1 <= rows.first && (key0 > last_lo || key1 < n_sink)) continue;
+        const int sl = slot0 + c, key0 = (sl < sink_slots ? sl : sl - sink_slots + from) * kSlotTok, key1 = key0 + kSlotTok - 1;
+        const bool there = sl < n_slots;
+        if (there && key1 <= row_first && (key0 > last_lo || key1 < n_sink)) continue;
         uint32_t r[16], m = 0;
-        if (there && key0 <= rows.last && (key1 > first_lo || key0 < n_sink)) {
+        if (there && key0 <= row_last && (key1 > first_lo || key0 < n_sink)) {
             ptx::tmem_ld_32x32b_x16(s_addr, r);
             const int at = pos - key0;                                                     // the row's own token, in the slot
             m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
@@ -502,12 +504,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
         uint32_t seq = V ? 1 : 0, n_seg = 0;
         bool ok = true;
         int pg = 0, pg_next = 0;
+        Keys keys = sg.keys;
+        const int32_t* table = nullptr;                              // the request's pages
+        int row0 = 0, kvh = 0, t_last = 0;                           // the layer's first page
         auto fetch = [&](int tt) -> int {                            // physical pages of a tile, one per lane (0..7)
             const int sl = tt * kTileSlots + lane;
-            return (lane < kTileSlots && sl < sg.keys.slots) ? p.c.page_table[(size_t)sg.u.b * p.c.max_pages + sg.keys.page(sl)] : 0;
+            return (lane < kTileSlots && sl < keys.slots) ? table[keys.page(sl)] : 0;
         };
         auto load_q = [&]() {
-            const int kvh = sg.u.hs / p.shares, head = kvh * p.c.G + (sg.u.hs - kvh * p.shares) * p.gs;
+            const int head = kvh * p.c.G + (sg.u.hs - kvh * p.shares) * p.gs;
             for (int g = 0; g < 2; ++g) {
                 if (!ptx::warp_wait(ctrl, &ctrl->q_empty[g], (n_seg & 1) ^ 1, 61)) { ok = false; return; }
                 if (ptx::elect_one()) {
@@ -521,33 +526,37 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
         };
         // what some row of the request sees (see causal::Request); the rest of V may be anything, and is taken as zeros
         int req_lo = 0, req_sink = 0, req_len = 0;
-        auto request = [&]() {
+        auto unit = [&]() {
+            keys = sg.keys;
+            t_last = sg.t_last;
+            table = p.c.page_table + (size_t)sg.u.b * p.c.max_pages;
+            row0 = sg.u.layer * p.c.layer_pages;
+            kvh = sg.u.hs / p.shares;
             req_len = sg.u.prefix + sg.u.n;
             req_lo = p.c.window > 0 ? min(max(0, sg.u.prefix - p.c.window + 1), req_len) : 0;
             req_sink = min(p.c.n_sink, req_lo);
         };
-        request();
+        unit();
         pg_next = fetch(t);
         if (V) load_q();
 #pragma unroll 1
         while (left > 0 && ok) {
             pg = pg_next;
-            if (t + 1 < sg.t_last) pg_next = fetch(t + 1);
+            if (t + 1 < t_last) pg_next = fetch(t + 1);
             const uint32_t st = seq % (uint32_t)n_stages;
             if (!ptx::warp_wait(ctrl, &ctrl->empty[st], ((seq / (uint32_t)n_stages) & 1) ^ 1, 60)) { ok = false; break; }
             uint8_t* const dst = ring + (size_t)st * C::kStageBytes;
             uint64_t* const bar = &ctrl->full[st];
-            const int sl0 = t * kTileSlots, n_sl = min(kTileSlots, sg.keys.slots - sl0), kvh = sg.u.hs / p.shares;
+            const int sl0 = t * kTileSlots, n_sl = min(kTileSlots, keys.slots - sl0);
             if (pg < 0 || pg >= p.c.num_pages) { causal::report(p.c.status, MIRROR_DEV_CHECK, 832); pg = 0; }
-            const int row0 = sg.u.layer * p.c.layer_pages;
             uint32_t partial = 0;                                    // V: slots with tokens that no row of the request sees
             if (V) {
-                const int key0 = sg.keys.page(sl0 + (lane & 7)) * kSlotTok;
+                const int key0 = keys.page(sl0 + (lane & 7)) * kSlotTok;
                 partial = __ballot_sync(0xffffffffu, lane < n_sl && (key0 + kSlotTok > req_len || (key0 < req_lo && key0 + kSlotTok > req_sink)));
                 if (partial) {
                     for (int k = 0; k < n_sl; ++k) {
                         if (!(partial >> k & 1)) continue;
-                        const int page = __shfl_sync(0xffffffffu, pg, k), base = sg.keys.page(sl0 + k) * kSlotTok;
+                        const int page = __shfl_sync(0xffffffffu, pg, k), base = keys.page(sl0 + k) * kSlotTok;
                         const uint8_t* const src = (const uint8_t*)p.c.v_pool + ((size_t)(row0 + page) * p.c.Hkv + kvh) * (size_t)C::kSlotBytes;
                         constexpr int kRowChunks = D / 8;
 #pragma unroll 1
@@ -585,10 +594,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             __syncwarp();
             seq += 2;
             --left;
-            if (++t == sg.t_last && left > 0) {
+            if (++t == t_last && left > 0) {
                 next_segment(sg, p, ctrl, left);
                 t = 0;
-                request();
+                unit();
                 pg_next = fetch(0);
                 if (V) load_q();
             }
@@ -626,17 +635,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
         Segment sg;
         first_segment(sg);
         StreamRows rows = stream_rows(p, sg, g);
-        int left = n_tiles, t = sg.t_first;                          // the tile whose Q K^T comes next
+        Keys keys = sg.keys;
+        int t_first = sg.t_first, t_last = sg.t_last;
+        int left = n_tiles, t = t_first;                          // the tile whose Q K^T comes next
         bool has_pv = false, pv_on = false, pv_last = false, started = false;
         int pv_sl = 0;
 #pragma unroll 1
         while (ok) {
-            const bool has_qk = left > 0;
+            const bool has_qk = left > 0, qk_on = has_qk && tile_seen(p, keys, rows, t), qk_last = has_qk && t + 1 == t_last;
+            const int qk_sl = has_qk ? slots_seen(keys, rows, t) : 0;
+            const uint32_t idesc_qk = ptx::umma_idesc_bf16(kRows, qk_sl * kSlotTok);
             uint32_t vst = 0, kst = 0;
             if (has_pv) vst = take();
             if (has_qk) {
                 kst = take();
-                if (t == sg.t_first) { wait(&ctrl->q_full[g], q_par, 63); q_par ^= 1; }
+                if (t == t_first) { wait(&ctrl->q_full[g], q_par, 63); q_par ^= 1; }
             }
             const uint32_t vb = v_lo + vst * (uint32_t)(C::kStageBytes >> 4);
             auto pv = [&](int k0, int k1) {
@@ -660,9 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             turn_par ^= 1;
             if (!ok) break;
             ptx::tc_fence_after();
-            const bool qk_on = has_qk && tile_seen(p, sg, rows, t), qk_last = has_qk && t + 1 == sg.t_last;
-            const int qk_sl = has_qk ? slots_seen(sg, rows, t) : 0;
-            const uint32_t idesc_qk = ptx::umma_idesc_bf16(kRows, qk_sl * kSlotTok), kb = k_lo + kst * (uint32_t)(C::kStageBytes >> 4);
+            const uint32_t kb = k_lo + kst * (uint32_t)(C::kStageBytes >> 4);
             if (ptx::elect_one()) {
                 if (has_pv) {
                     if (pv_on) pv(kTileSlots / 2, pv_sl);
@@ -689,10 +700,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             pv_last = qk_last;
             pv_sl = qk_sl;
             --left;
-            if (++t == sg.t_last && left > 0) {
+            if (++t == t_last && left > 0) {
                 next_segment(sg, p, ctrl, left);
                 rows = stream_rows(p, sg, g);
-                t = 0;
+                keys = sg.keys;
+                t_last = sg.t_last;
+                t = t_first = 0;
             }
         }
     } else {
@@ -726,22 +739,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             const bool row_ok = it < p.nt && tok < sg.u.n && hg < p.c.G;
             const bool warp_has_rows = __any_sync(0xffffffffu, row_ok);
             float off = row_ok ? -INFINITY : 1e30f, l_run = 0.f;
+            const Keys keys = sg.keys;
+            const int t_last = sg.t_last;
             bool redone = false, any_tile = false;                   // any_tile: the accumulator holds something
 #pragma unroll 1
-            for (int t = sg.t_first; t < sg.t_last; ++t) {
-                const bool on = tile_seen(p, sg, rows, t);
+            for (int t = sg.t_first; t < t_last; ++t) {
+                const bool on = tile_seen(p, keys, rows, t);
                 if (!ptx::warp_wait(ctrl, &ctrl->s_full[grp], s_par, 68)) { ok = false; break; }
                 s_par ^= 1;
                 ptx::tc_fence_after();
                 if (warp_has_rows && on) {
-                    const int key0 = sg.keys.page(t * kTileSlots) * kSlotTok;
-                    const bool whole_tile = (t + 1) * kTileSlots <= sg.keys.slots && sg.keys.page(t * kTileSlots + kTileSlots - 1) * kSlotTok + kSlotTok - 1 <= rows.first &&
+                    const int key0 = keys.page(t * kTileSlots) * kSlotTok;
+                    const bool whole_tile = (t + 1) * kTileSlots <= keys.slots && keys.page(t * kTileSlots + kTileSlots - 1) * kSlotTok + kSlotTok - 1 <= rows.first &&
                                             (p.c.window == 0 || key0 > rows.last - p.c.window);
                     // Two halves of 64 scores, one copy of the code (the second left out where no row sees it).  P of a half goes over S columns
                     // that have been read.
-                    const int halves = slots_seen(sg, rows, t) > kTileSlots / 2 ? 2 : 1;
+                    const int halves = slots_seen(keys, rows, t) > kTileSlots / 2 ? 2 : 1;
                     // The offset is set by the first tile in which the row sees anything (before that every P was 0).
-                    if (!whole_tile) mask_tile(s_addr, t * kTileSlots, halves * (kTileSlots / 2), sg.keys, pos, rows, p.c.window, p.c.n_sink);
+                    if (!whole_tile) mask_tile(s_addr, t * kTileSlots, halves * (kTileSlots / 2), keys.sink_slots, keys.from, keys.slots, pos, rows.first, rows.last, p.c.window, p.c.n_sink);
                     if (__any_sync(0xffffffffu, off == -INFINITY)) {
                         const float mx = tile_max(s_addr, 2 * halves);
                         if (off == -INFINITY) off = mx * sc;       // (-inf when nothing is visible yet)
@@ -809,6 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             const int slot = sg.t_first > 0 ? 0 : 1;                 // a unit that began before this CTA's range uses slot 0
             float* const rec = p.c.partial + (((size_t)blockIdx.x * 2 + slot) * 2 + grp) * kRowW * kRows + row;
             left -= sg.t_last - sg.t_first;
+            if (left > 0) next_segment(sg, p, ctrl, left);           // (while the last P V is running)
             if (!ptx::warp_wait(ctrl, &ctrl->o_full[grp], o_par, 70)) { ok = false; break; }
             o_par ^= 1;
             ptx::tc_fence_after();
@@ -842,7 +858,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             }
             // (the stream's next P V waits for a P that its own warps write after this)
             ptx::tc_fence_before();
-            if (left > 0) next_segment(sg, p, ctrl, left);
         }
     }
 
