@@ -390,7 +390,10 @@ struct Cfg {
 // and little code: most of a tile's slots are seen by all rows, or by none, and what runs once per unit is bound by the fetch of its
 // instructions (32 columns at a time, unrolled, with the maximum taken on the way: 4400 cycles, this and tile_max 2500).
 __device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, int slots, int sink_slots, int from, int n_slots, int pos, int row_first, int row_last, int window, int n_sink) {
-    const int first_lo = window > 0 ? row_first - window : -1, last_lo = window > 0 ? row_last - window : -1;     // (what lies up to there is out of the window)
+    // (what lies up to there is out of the window; without one, or with one past all positions, nothing does)
+    window = window == 0 ? 1 << 30 : min(window, 1 << 30);
+    const int first_lo = row_first - window, last_lo = row_last - window;
+    auto bits = [](int n) { return 1u << min(max(n, 0), 16); };
 #pragma unroll 1
     for (int c = 0; c < slots; ++c, s_addr += 16) {
         const int sl = slot0 + c, key0 = (sl < sink_slots ? sl : sl - sink_slots + from) * kSlotTok, key1 = key0 + kSlotTok - 1;
@@ -399,13 +402,8 @@ __device__ __noinline__ void mask_tile(uint32_t s_addr, int slot0, int slots, in
         uint32_t r[16], m = 0;
         if (there && key0 <= row_last && (key1 > first_lo || key0 < n_sink)) {
             ptx::tmem_ld_32x32b_x16(s_addr, r);
-            const int at = pos - key0;                                                     // the row's own token, in the slot
-            m = at >= 15 ? 0xffffu : at < 0 ? 0u : (2u << at) - 1u;
-            if (window > 0) {
-                const int lo = at - window + 1, sk = n_sink - key0;
-                const uint32_t in = lo <= 0 ? 0xffffu : lo > 15 ? 0u : 0xffffu & ~((1u << lo) - 1u);
-                m &= in | (sk >= 16 ? 0xffffu : sk <= 0 ? 0u : (1u << sk) - 1u);
-            }
+            const int n = pos + 1 - key0;                                                  // of the slot's tokens those ahead of the row's, and its own
+            m = (bits(n) - 1u) & (0u - bits(n - window) | (bits(n_sink - key0) - 1u));
             tmem_ld_wait16(r);
         }
 #pragma unroll

@@ -64,6 +64,12 @@ def test_prompts_under_a_window(window, sinks, d):
     check_attention(make(2, 2, d), Case(2, 2, d, [0, 700, 33], [400, 129, 256], window=window, sinks=sinks, seed=window + 1), True)
 
 
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (7, 2 ** 31 - 1), (2 ** 30 + 5, 3)])
+def test_the_widest_windows_and_sinks(window, sinks):
+    check_attention(make(8, 2, 64), Case(8, 2, 64, LENS, [1] * 10, window=window, sinks=sinks, seed=3), False)
+    check_attention(make(8, 2, 64), Case(8, 2, 64, LENS, COUNTS, window=window, sinks=sinks, seed=4), True)
+
+
 def test_prompts_of_every_length_around_a_tile():
     for n in (17, 31, 32, 33, 63, 64, 65, 127, 128, 129):
         check_attention(make(4, 1, 64), Case(4, 1, 64, [n, 0, 128 - n % 128], [n, n + 1, 1], seed=n), True)
