@@ -43,6 +43,7 @@ constexpr int kBins = 2048;
 constexpr float kBinsPerNat = 64.f;
 constexpr int kList = 2048;                   // candidates that the leader ranks
 constexpr int kShort = 256;                   // so few that each is compared with each
+constexpr int kDeep = 48;                     // ids of a bin, above which pairs are sorted
 constexpr int kMaxCluster = 16;
 constexpr int kGroup = 4;                     // a group: this many of a thread's loads, 16 ids
 constexpr int kTable = 64;
@@ -91,6 +92,7 @@ struct alignas(16) Shared {
     u64 cut_key;                              // composite key of the last kept id
     u64 kept, kept_mass;                      // ids of its front, their mass
     u64 base;
+    uint32_t key_first, key_last;             // of the list that is sorted: logits
     int last_bin, list_at;                    // written by the leader
     int n_list, n_all;                        // ids up to last_bin, and in all bins
     int bin_k, bin_p;                         // ... the bins in which Top-k and (estimated) Top-p end
@@ -177,27 +179,64 @@ __device__ __forceinline__ u64 block_scan(Shared& s, const u64 (&w)[kPer], u64& 
     return __shfl_sync(0xffffffffu, all, kWarps - 1);
 }
 
-// list[0 .. n) in ascending order: sorted into bins over the logits from `hi` down, `scale` of them to a nat of it, and within a bin by
-// comparing all with all.
-template <int kThreads, int kPer>
-__device__ __noinline__ void sort_list(Shared& s, int n, float hi, float scale) {
-    constexpr int kBinsPer = kBins / kThreads;
+// list[0 .. n) in ascending order, whatever it holds: log2(n)^2 / 2 rounds of compared pairs.
+template <int kThreads>
+__device__ __noinline__ void sort_pairs(Shared& s, int n) {
     const int tid = threadIdx.x;
-    auto place = [&](u64 key) { return (int)fminf(fmaxf((hi - logit_of(key)) * scale, 0.f), (float)(kBins - 1)); };
+    int N = 2;
+    while (N < n) N <<= 1;
+    for (int i = n + tid; i < N; i += kThreads) s.list[i] = ~0ull;
+    __syncthreads();
+    for (int k = 2; k <= N; k <<= 1)
+        for (int d = k >> 1; d > 0; d >>= 1) {
+            for (int i = tid; i < N / 2; i += kThreads) {
+                const int a = 2 * i - (i & (d - 1));
+                const u64 x = s.list[a], y = s.list[a + d];
+                if ((x > y) == ((a & k) == 0)) { s.list[a] = y; s.list[a + d] = x; }
+            }
+            __syncthreads();
+        }
+}
+// The same: sorted into bins over the logits' range, and within a bin by comparing all with all.  (Many equal logits, or one far away from
+// the others, make bins so deep that pairs are sooner.)
+template <int kThreads, int kPer>
+__device__ __noinline__ void sort_list(Shared& s, int n) {
+    constexpr int kBinsPer = kBins / kThreads;
+    const int tid = threadIdx.x, lane = tid & 31;
     __syncthreads();
     for (int i = tid; i < kBins; i += kThreads) s.hist[i] = 0;
-    __syncthreads();
+    if (tid == 0) { s.key_first = ~0u; s.key_last = 0; }
     u64 key[kPer];
+    uint32_t k0 = ~0u, k1 = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         key[j] = tid + j * kThreads < n ? s.list[tid + j * kThreads] : ~0ull;
-        if (tid + j * kThreads < n) atomicAdd(&s.hist[place(key[j])], 1u);
+        if (tid + j * kThreads < n) { k0 = min(k0, (uint32_t)(key[j] >> 32)); k1 = max(k1, (uint32_t)(key[j] >> 32)); }
     }
+    __syncthreads();
+    k0 = __reduce_min_sync(0xffffffffu, k0);
+    k1 = __reduce_max_sync(0xffffffffu, k1);
+    if (lane == 0) { atomicMin(&s.key_first, k0); atomicMax(&s.key_last, k1); }
+    __syncthreads();
+    const float hi = logit_of((u64)s.key_first << 32), span = hi - logit_of((u64)s.key_last << 32);
+    const float scale = span > 0.f && span < INFINITY ? (float)(kBins - 1) / span : 0.f;
+    auto place = [&](u64 k) { return (int)fminf(fmaxf((hi - logit_of(k)) * scale, 0.f), (float)(kBins - 1)); };
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (tid + j * kThreads < n) atomicAdd(&s.hist[place(key[j])], 1u);
     __syncthreads();
     {
         u64 cnt[kBinsPer], before;
+        u64 most = 0;
 #pragma unroll
-        for (int j = 0; j < kBinsPer; ++j) cnt[j] = s.hist[tid * kBinsPer + j];
+        for (int j = 0; j < kBinsPer; ++j) {
+            cnt[j] = s.hist[tid * kBinsPer + j];
+            most = max(most, cnt[j]);
+        }
+        if (__syncthreads_or(most > (u64)kDeep)) {
+            sort_pairs<kThreads>(s, n);
+            return;
+        }
         block_scan<kThreads>(s, cnt, before);
 #pragma unroll
         for (int j = 0; j < kBinsPer; ++j) {
@@ -653,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             auto finish = [&](auto per) {
                 constexpr int P = decltype(per)::value;          // ids of a thread
                 if (P == 1) sort_short(s, n_list);
-                else sort_list<kThreads, P>(s, n_list, weigh.hi, weigh.hi - from > 0.f && !max_inf ? (float)(kBins - 1) / (weigh.hi - from) : 0.f);
+                else sort_list<kThreads, P>(s, n_list);
                 u64 key[P], w[P], sel[P], before;
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
@@ -839,8 +878,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 gather([&](int c) { return (int)(s.sum[was][c][0] >> 32); });
                 if (rank == 0) {
                     const int n = (int)n_in;
-                    // (the bin's range; the last bin is open, and goes by comparing)
-                    sort_list<kThreads, kPer>(s, n, weigh.hi - (float)b * T * (1.f / kBinsPerNat), max_inf || b == kBins - 1 ? 0.f : (float)(kBins - 1) * kBinsPerNat * inv_T);
+                    sort_list<kThreads, kPer>(s, n);
                     if (tid == 0) s.list_at = n - 1;
                     u64 w[kPer], before;
 #pragma unroll
