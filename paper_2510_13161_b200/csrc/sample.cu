@@ -810,7 +810,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             auto end_of = [&](int b, bool of_all, auto done) -> u64 {
                 u64 n0, m0, n_in, all = 0;
                 u64 lo = 0, hi = ~0ull;                          // (what is known of the key where the guess is off again and again)
-                bool far = false;
+                bool far = false, early = false;
                 int was = 0;
                 for (int again = 0;; ++again) {
                     // what lies ahead of the bin, and the bin itself into the leader's list
@@ -856,7 +856,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     if (rest) all = a.t;
                     ahead_bin = b;
                     known = false;
-                    const bool early = n0 > 0 && done(n0, m0, all), late = b < kBins - 1 && !done(n0 + n_in, m0 + a.o, all);
+                    early = n0 > 0 && done(n0, m0, all);
+                    const bool late = b < kBins - 1 && !done(n0 + n_in, m0 + a.o, all);
                     far = (early || late) && again >= 3;
                     // (the bin's own keys, or all ahead of it, or all behind it)
                     if (far || n_in > (u64)kList) {
@@ -868,10 +869,24 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 }
                 if (far) ahead_bin = -1;
                 if (far || n_in > (u64)kList) {
+                    // the logit first, then the id; what lies ahead of `lo` is known, so few ids are weighed
+                    u64 n_lo = early ? 0ull : n0, m_lo = early ? 0ull : m0;
                     while (lo < hi) {
-                        const u64 mid = lo + ((hi - lo) >> 1);
-                        const Sums a = front(mid);
-                        if (done(a.n, a.m, all)) hi = mid; else lo = mid + 1;
+                        const uint32_t l0 = (uint32_t)(lo >> 32), l1 = (uint32_t)(hi >> 32);
+                        if (l0 == l1) hi = min(hi, ((u64)l0 << 32) | (uint32_t)(p.V - 1));
+                        const u64 mid = l0 < l1 ? ((u64)(l0 + ((l1 - l0) >> 1)) << 32) | 0xffffffffull : lo + ((hi - lo) >> 1);
+                        const Sums a = all_sums([&](float l, int i, Sums& a) {
+                            if (!may(l)) return;
+                            const u64 key = key_of(l, first + i);
+                            if (key >= lo && key <= mid) { ++a.n; a.m += weigh(l); }
+                        });
+                        if (done(n_lo + a.n, m_lo + a.m, all)) {
+                            hi = mid;
+                        } else {
+                            lo = mid + 1;
+                            n_lo += a.n;
+                            m_lo += a.m;
+                        }
                     }
                     return lo;
                 }
