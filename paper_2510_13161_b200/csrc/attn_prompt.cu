@@ -23,8 +23,8 @@
 //
 // What bounds it: the chain of a step (4000 cycles for two streams' 128 x 128 at d = 128, 3430 at d = 64; the tensor pipe is busy for half of them), units'
 // starts and ends (4 to 5 thousand cycles each) where prompts are short, and power where they are long.  Measured on a B200: 2048 rows behind
-// 30720 tokens, 64 / 8 heads of 128: 2.0 ms (1070 TFLOP/s), 2.3 run back to back; 2048 rows from 0, 40 / 8 heads of 128: 67 us; seven ragged chunks, 32 / 8
-// heads of 64 under a window of 1000: 190 us.
+// 30720 tokens, 64 / 8 heads of 128: 2.0 ms (1070 TFLOP/s), 2.2 run back to back; 2048 rows from 0, 40 / 8 heads of 128: 61 us; seven ragged chunks, 32 / 8
+// heads of 64 under a window of 1000: 175 us.
 #include <math.h>
 
 #include <algorithm>
