@@ -53,7 +53,7 @@ static_assert(kMaxPart / (4 * kGroup) <= 2 * kList && kMaxPart % (1024 * kGroup)
 static_assert(kBins == kList, "a thread has as many bins as candidates");
 
 struct SampleParams {
-    int V, M, part;                           // part: ids of a CTA, a multiple of 128 per warp
+    int V, part;                           // part: ids of a CTA, a multiple of 128 per warp
     int shift;                                // S
     int id_shift;                             // ids >> id_shift are less than kList
     int off_bits, off_shift;                  // of a histogram word: see pack_off
@@ -1086,7 +1086,7 @@ extern "C" mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int
         return MIRROR_ERR_ARG;
     MIRROR_CUDA_OK(cudaSetDevice(ctx->device));
     SampleParams p;
-    p.V = V; p.M = M; p.ld = ld;
+    p.V = V; p.ld = ld;
     int bits = 0;
     while ((1ll << bits) < V) ++bits;
     p.shift = 62 - bits < 51 ? 62 - bits : 51;                   // (a weight has to fit a double's 52 bits)
