@@ -205,6 +205,22 @@ def test_out_of_place_equals_in_place():
     assert torch.equal(x, want["probs"]) and torch.equal(tok, want["token"])
 
 
+@pytest.mark.parametrize("M,V", [(2, 30004), (60, 30004), (60, 30001), (300, 700)])
+@pytest.mark.parametrize("k,p", [(50, 1.0), (0, 0.9), (3000, 0.7), (0, 1.0)])
+@pytest.mark.parametrize("what", ["probs", "logits"])
+def test_every_way_in_place(M, V, k, p, what):
+    m = make(2, 2, 64, vocab=V)
+    x = torch.from_numpy(logits_of(M, V, V + k, std=1.0)).cuda()
+    u, pd, kd = torch.rand(M, device="cuda"), torch.full((M,), p, device="cuda"), torch.full((M,), k, dtype=torch.int32, device="cuda")
+    want = m.mirror_sample(x, u, top_k=kd, top_p=pd, want_probs=what == "probs", want_logits=what == "logits")
+    tok = torch.empty(M, dtype=torch.int32, device="cuda")
+    out = (x.data_ptr(), None) if what == "probs" else (None, x.data_ptr())
+    assert m.lib.mirror_sample(m._ctx, x.data_ptr(), V, M, None, kd.data_ptr(), pd.data_ptr(), None, u.data_ptr(), tok.data_ptr(), None, None, *out,
+                               torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(x, want[what]) and torch.equal(tok, want["token"])
+
+
 def test_captured_and_replayed():
     m = make(2, 2, 64, vocab=3001)
     x = torch.from_numpy(logits_of(4, 3001, 10)).cuda()
