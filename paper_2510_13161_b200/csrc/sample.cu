@@ -29,6 +29,7 @@
 #include <math.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "mirror_internal.h"
 
@@ -287,6 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     const int n_mine = max(0, min(p.part, p.V - first));
     const int per_warp = p.part / kWarps, w0 = warp * per_warp, w1 = min(w0 + per_warp, (n_mine + 3) & ~3);
     Shared* const lead = cluster.map_shared_rank(&s, 0);
+    auto started = cluster.barrier_arrive();
 
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
@@ -349,6 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     for (int o = 16; o; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     if (lane == 0) s.warp_sum[warp][0] = __float_as_uint(mx);
     __syncthreads();
+    // (every CTA of the cluster has started: its shared memory may be written to.  One without ids is here long before the others.)
+    cluster.barrier_wait(std::move(started));
     if (tid < kWarps) {
         mx = __uint_as_float((uint32_t)s.warp_sum[tid][0]);
 #pragma unroll

@@ -267,3 +267,17 @@ def test_refusals():
     big = make(2, 2, 64, vocab=16 * 40960 + 1)
     assert big.lib.mirror_sample(big._ctx, x.data_ptr(), 16 * 40960 + 1, 1, None, None, None, None, u.data_ptr(), u.data_ptr(), None, None, None, None, None) == 2
     assert binding.MirrorError
+
+
+@pytest.mark.parametrize("V", [2049, 4097, 8193, 8200])
+@pytest.mark.parametrize("M", [1, 9, 30])
+def test_clusters_whose_last_ctas_have_few_ids_or_none(V, M):
+    """Rows so short that the last CTAs of a cluster have nothing to load and are through with it long before the others have begun: call
+    after call, the same tokens."""
+    x = logits_of(M, V, V + M)
+    check(x, k=20, seed=V)
+    m = make(2, 2, 64, vocab=V)
+    xd, u = torch.from_numpy(x).cuda(), torch.rand(M, device="cuda", generator=torch.Generator(device="cuda").manual_seed(V))
+    want = [int(O.sample_row(x[r], u=float(u[r]))[0]) for r in range(M)]
+    got = [m.mirror_sample(xd, u)["token"] for _ in range(200)]
+    assert (torch.stack(got).cpu() == torch.tensor(want, dtype=torch.int32)).all()
