@@ -827,15 +827,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
             o_par ^= 1;
             ptx::tc_fence_after();
             if (warp_has_rows) {
-                const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-                const float w = off == -INFINITY || !any_tile ? 0.f : whole ? inv : 1.f;
+                // (a sum that is no number, or 0 where every score is -inf, makes the row NaN, as in the merge and for single tokens)
+                const float inv = 1.f / l_run;
+                // An accumulator that no P V wrote may hold anything, and a part in which the row saw nothing has no weight: neither is read.
+                const bool nothing = !any_tile || (!whole && off == -INFINITY);
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t r[32];
                     ptx::tmem_ld_32x32b_x32(o_addr + (uint32_t)c, r);
                     tmem_ld_wait32(r);
-                    // (an accumulator that no P V wrote may hold anything: a weight of 0 does not read it)
-                    if (w == 0.f) {
+                    if (nothing) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) r[j] = 0u;
                     }
@@ -843,8 +844,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prompt_kernel(const __grid_c
 #pragma unroll
                         for (int j = 0; j < 32; ++j) rec[(size_t)(c + j) * kRows] = __uint_as_float(r[j]);
                     } else if (row_ok) {
-                        store32(orow + c, r, w, p.wide_out != 0);
-                        store32(orow + c + 16, r + 16, w, p.wide_out != 0);
+                        store32(orow + c, r, inv, p.wide_out != 0);
+                        store32(orow + c + 16, r + 16, inv, p.wide_out != 0);
                     }
                 }
                 if (!whole) {

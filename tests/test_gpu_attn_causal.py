@@ -1,4 +1,5 @@
 """mirror_attn_causal against the oracle in 64 bits; everything that no row sees is NaN in the cache."""
+import numpy as np
 import pytest
 import torch
 
@@ -228,3 +229,51 @@ def test_refusals():
     m2 = make(4, 2, 64)
     import ctypes as C
     assert m2.lib.mirror_attn_causal(m2._ctx, C.byref(kv), C.byref(rows), 0, 0, q.data_ptr(), q.data_ptr(), None, None) == 4        # no workspace
+
+
+SPOILED = [(8, 2, LENS, [1] * 10, 0, 0, False), (8, 2, LENS, [1, 2, 3, 4, 4, 2, 4, 4, 0, 3], 0, 0, False), (8, 1, [20000], [2], 0, 0, False), (8, 2, LENS, [2] * 10, 40, 3, False),
+           (8, 2, LENS, [1, 100, 16, 0, 300, 33, 128, 15, 257, 64], 0, 0, True), (8, 2, LENS, [1, 100, 16, 0, 300, 33, 128, 15, 257, 64], 40, 3, True),
+           (8, 1, [9000], [40], 0, 0, True), (4, 4, [0, 3000], [1500, 20], 0, 0, True)]
+
+
+@pytest.mark.parametrize("hq,hkv,lens,counts,window,sinks,p_rounded", SPOILED)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("what", ["query nan", "query inf", "key nan", "key inf", "key -inf", "all -inf"])
+def test_scores_that_are_no_numbers(hq, hkv, lens, counts, window, sinks, p_rounded, d, what):
+    """NaN or an infinity in a query, or in a key that some rows see: the rows whose softmax has no value are NaN, as in 64 bits, whether
+    their unit was cut or not, and all others are as they would be."""
+    m = make(hq, hkv, d)
+    c = Case(hq, hkv, d, lens, counts, window=window, sinks=sinks, seed=31)
+    s = 1 / np.sqrt(d)
+    b = int(np.argmax(np.asarray(lens) + 1000 * np.asarray(counts)))
+    row, pos = int(c.start[b]) + counts[b] // 2, lens[b] + counts[b] // 2                       # a row in the middle, and its own key
+    if what.startswith("query"):
+        c.q[0, row, 1, 5] = float(what.split()[1])
+    elif what.startswith("key"):
+        c.k[0, c.table[b, pos // PAGE], 0, pos % PAGE, 5] = float(what.split()[1])
+    else:                                                        # one row's query meets only keys of the other sign
+        c.q[0, row, 1] = 0.0
+        c.q[0, row, 1, 5] = float("-inf")
+        for j in range(lens[b] + counts[b]):
+            page = c.table[b, j // PAGE]
+            if page < c.k.shape[1]:
+                c.k[0, page, 0, j % PAGE, 5] = c.k[0, page, 0, j % PAGE, 5].abs() + 0.125
+    largest = lambda t: float(t.float().nan_to_num(0.0, 0.0, 0.0).norm(dim=-1).max())  # noqa: E731
+    moved = d * 2.0 ** -24 * s * largest(c.q) * largest(c.k)
+    kv, rows = c.device(m)
+    lse = torch.full((1, c.R, hq), 7.0, device="cuda")
+    out = m.mirror_attn_causal(kv, rows, c.q.cuda(), window=window, sinks=sinks, lse_out=lse)
+    torch.cuda.synchronize()
+    assert m.device_status() == (0, 0)
+    with np.errstate(invalid="ignore"):
+        want, want_lse, spread = c.expect(0, s)
+    got, gl, none = out[0].double().cpu().numpy(), lse[0].double().cpu().numpy(), np.isnan(want)
+    assert not none.all() and np.array_equal(none.any(-1), none.all(-1))
+    assert np.array_equal(np.isnan(got), none)
+    assert not np.isfinite(gl[none.all(-1)]).any()
+    # (tolerances of check_attention)
+    ok = ~none
+    tol = 2.0 ** -8 * np.abs(want) + ((2.0 ** -8 if p_rounded else 2.0 ** -15) + 2 * moved + 1e-6) * spread + 1e-30
+    assert (np.abs(got - want)[ok] <= tol[ok]).all()
+    ok = ~none.all(-1)
+    assert (np.abs(gl - want_lse)[ok] <= moved + 2e-6 * (1 + np.abs(want_lse[ok]))).all()
