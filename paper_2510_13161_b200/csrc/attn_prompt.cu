@@ -139,7 +139,7 @@ struct Ctrl {
     int first_t, n_tiles, whole;
     int cut, too_long;                                  // it begins inside a unit; more tiles than 31 bits count
     int makespan, ends[2];
-    int scan[kThreads / 32];
+    uint32_t scan[kThreads / 32];
     int* status;
     long long wait_limit;
     uint32_t tmem_base;
@@ -175,17 +175,18 @@ __device__ __noinline__ void next_segment(Segment& s, const PromptParams& p, con
 // It is made twice as far as its inputs are concerned: ahead of the kernel in front, from whatever the lengths are then (nothing but this
 // CTA's shared memory is written), and once that kernel is through the lengths are read again: hardly ever has one changed, and then the
 // plan is made anew.  (It takes 4 us, most of them for code that runs once.)
-__device__ int block_scan(int v, int* s_warp, int* total) {              // inclusive, over the block
+// Tiles, inclusive over the block.  (A page table has at most 2^26 entries, a pair at most 2^23 tiles: those of a block fit 32 bits.)
+__device__ uint32_t block_scan(uint32_t v, uint32_t* s_warp, uint32_t* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, v, o);
+        const uint32_t t = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += t;
     }
     __syncthreads();
     if (lane == 31) s_warp[warp] = v;
     __syncthreads();
-    int before = 0, all = 0;
+    uint32_t before = 0, all = 0;
     for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) before += s_warp[w];
         all += s_warp[w];
@@ -246,16 +247,16 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
         return u;
     };
     Unit mine = {};
-    int total = 0, cum = 0;                              // tiles of all pairs; of those before `mine`
+    long long total = 0, cum = 0;                        // tiles of all pairs; of those before `mine`
     for (int c0 = 0; c0 < pairs; c0 += kThreads) {
         mine = {};
         if (c0 + tid < pairs) mine = pair(c0 + tid);
-        int all;
-        cum = total + block_scan(mine.tiles, ctrl->scan, &all) - mine.tiles;
+        uint32_t all;
+        cum = total + block_scan((uint32_t)mine.tiles, ctrl->scan, &all) - mine.tiles;
         total += all;
     }
     const int lh = p.c.L * p.n_hs;
-    const long long seq = (long long)lh * total, units = (long long)lh * pairs;
+    const long long seq = lh * total, units = (long long)lh * pairs;
     if (seq >= (1ll << 31)) {
         if (tid == 0) ctrl->too_long = 1;
         return;
@@ -327,17 +328,17 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
     const int used = (int)min((long long)p.n_cta, seq);
     const int tol = (int)min((long long)kSnapTiles, seq / used >> 2);
     long long x0 = cta >= used ? seq : seq * cta / used, x1 = cta + 1 >= used ? seq : seq * (cta + 1) / used;
-    const int per = total;                               // tiles of one (layer, head)
+    const int per = (int)total;                          // tiles of one (layer, head)
     const int lh0 = (int)(x0 / per), rem0 = (int)(x0 - (long long)lh0 * per), rem1 = (int)(x1 % per);
     int* const s_ends = ctrl->ends;
     if (tid == 0) { s_ends[0] = (int)x0; s_ends[1] = (int)x1; }
-    int seen = 0;
+    long long seen = 0;
     for (int c0 = 0; c0 < pairs; c0 += kThreads) {
         if (pairs > kThreads) {                          // (a second time: the first kept the last pairs only)
             mine = {};
             if (c0 + tid < pairs) mine = pair(c0 + tid);
-            int all;
-            cum = seen + block_scan(mine.tiles, ctrl->scan, &all) - mine.tiles;
+            uint32_t all;
+            cum = seen + block_scan((uint32_t)mine.tiles, ctrl->scan, &all) - mine.tiles;
             seen += all;
         }
         __syncthreads();
@@ -345,7 +346,7 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
             // (this pair's tiles lie in front of both boundaries' places within their head, or hold them)
             if (x0 < seq && rem0 >= cum && rem0 < cum + mine.tiles) {
                 Unit u = mine;
-                int t = rem0 - cum, at = lh0;
+                int t = rem0 - (int)cum, at = lh0;
                 if (t <= tol) {
                     s_ends[0] = (int)x0 - t;
                     t = 0;
@@ -362,7 +363,7 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
                 ctrl->first_t = t;
             }
             if (x1 < seq && rem1 >= cum && rem1 < cum + mine.tiles) {
-                const int t = rem1 - cum;
+                const int t = rem1 - (int)cum;
                 if (t <= tol) s_ends[1] = (int)x1 - t;
                 else if (mine.tiles - t <= tol) s_ends[1] = (int)x1 + mine.tiles - t;
             }

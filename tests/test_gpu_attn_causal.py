@@ -277,3 +277,22 @@ def test_scores_that_are_no_numbers(hq, hkv, lens, counts, window, sinks, p_roun
     assert (np.abs(got - want)[ok] <= tol[ok]).all()
     ok = ~none.all(-1)
     assert (np.abs(gl - want_lse)[ok] <= moved + 2e-6 * (1 + np.abs(want_lse[ok]))).all()
+
+
+@pytest.mark.parametrize("hkv,n", [(1, 6000), (1, 8300), (2, 6000)])
+def test_more_tiles_than_can_be_counted(hkv, n):
+    """A page table of 2^27 tokens and thousands of rows behind them: 1048511 tiles for each pair of row tiles (two rows of 128 heads, or four of
+    64 a KV head), which over the pairs and heads is past 2^31, or past 2^32.  Such a call is reported, and its rows are left as they are."""
+    m = make(128, hkv, 64)
+    pools = [torch.zeros((1, 4, hkv, PAGE, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    pages = 1 << 23
+    prefix = pages * PAGE - n
+    tiles = n // (2 * hkv) * (prefix // 128) * hkv               # at least
+    assert tiles > 1 << (32 if n == 8300 else 31)
+    kv = m.kv(*pools, torch.zeros((1, pages), dtype=torch.int32, device="cuda"), torch.tensor([prefix], dtype=torch.int32, device="cuda"))
+    q = torch.zeros((1, n, 128, 64), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((1, n, 128), 7.0, device="cuda")
+    m.mirror_attn_causal(kv, m.rows(None, n, n, 1), q, out=out, lse_out=lse)
+    torch.cuda.synchronize()
+    assert m.device_status() == (6, 833)
+    assert (out == 7.0).all() and (lse == 7.0).all()
