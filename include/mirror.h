@@ -318,7 +318,8 @@ typedef struct {
     int batch;                /* B requests, at most 1024 */
     int n_rows;               /* R: rows of the tensors, those behind the last request's included (they are left as they are) */
     int max_rows;             /* upper bound of a request's rows; 1: single tokens */
-    const int32_t* row_start; /* device [B + 1], not decreasing: request b has the rows row_start[b] .. row_start[b+1] - 1;
+    const int32_t* row_start; /* device [B + 1], not decreasing (where it does, mirror_attn_causal reports it, and its output is not defined):
+                                 request b has the rows row_start[b] .. row_start[b+1] - 1;
                                  NULL: every request has max_rows rows (R >= B * max_rows) */
 } mirror_rows;
 

@@ -214,6 +214,8 @@ __device__ __forceinline__ bool load_rows(const PromptParams& p, const Scratch& 
 __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* mem) {
     const int tid = threadIdx.x, lane = tid & 31, B = p.c.B, cta = blockIdx.x;
     const Scratch x(mem, B);
+    // (sums stop one above what rows in ascending order come to, of which each belongs to one request)
+    const int most_pairs = p.c.R / (2 * p.nt) + B + 1;
     for (int b = tid; b < B; b += kThreads) x.base[b + 1] = (x.n[b] + 2 * p.nt - 1) / (2 * p.nt);
     if (tid == 0) { x.base[0] = 0; ctrl->makespan = 0; ctrl->n_tiles = 0; ctrl->whole = 0; ctrl->cut = 0; ctrl->too_long = 0; }
     __syncthreads();
@@ -224,15 +226,16 @@ __device__ __noinline__ void make_plan(const PromptParams& p, Ctrl* ctrl, int* m
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int t = __shfl_up_sync(0xffffffffu, v, o);
-                if (lane >= o) v += t;
+                if (lane >= o) v = min(v + t, most_pairs);
             }
-            if (b0 + lane < B) x.base[b0 + lane + 1] = acc + v;
-            acc += __shfl_sync(0xffffffffu, v, 31);
+            v = min(acc + v, most_pairs);
+            if (b0 + lane < B) x.base[b0 + lane + 1] = v;
+            acc = __shfl_sync(0xffffffffu, v, 31);
         }
     }
     __syncthreads();
     const int pairs = x.base[B];
-    if (pairs == 0) return;
+    if (pairs == 0 || pairs == most_pairs) return;       // (rows that are not in order have been reported)
     auto pair = [&](int c) {                             // pair number c, in the order of the rows
         int lo = 0, hi = B - 1;                          // the first b with base[b + 1] > c
         while (lo < hi) {

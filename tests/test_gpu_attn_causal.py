@@ -296,3 +296,22 @@ def test_more_tiles_than_can_be_counted(hkv, n):
     torch.cuda.synchronize()
     assert m.device_status() == (6, 833)
     assert (out == 7.0).all() and (lse == 7.0).all()
+
+
+def test_rows_that_are_not_in_order():
+    """Every other request claims all rows: reported, and no plan of 32 times the work is made."""
+    m = make(4, 1, 64)
+    B, R = 64, 4096
+    pools = [torch.zeros((1, 4, 1, PAGE, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    kv = m.kv(*pools, torch.zeros((B, 300), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda"))
+    start = torch.tensor([0, R] * (B // 2) + [0], dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, R, 4, 64), dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    m.mirror_attn_causal(kv, m.rows(start, R, R), q, out=out)
+    torch.cuda.synchronize()
+    assert m.device_status() == (6, 830)
+    assert (out == 7.0).all()
+    start.copy_(torch.arange(B + 1, dtype=torch.int32) * (R // B))
+    m.mirror_attn_causal(kv, m.rows(start, R, R), q, out=out)
+    torch.cuda.synchronize()
+    assert m.device_status() == (0, 0) and (out == 0.0).all()
