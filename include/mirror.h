@@ -395,8 +395,9 @@ mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mir
  *               mirror_accept_select takes for a target under the same filters
  * All three filters keep a front of the ranks (logit descending, id ascending), at least the first.  NaN and -inf are never kept (a row of
  * nothing else: token -1, logprob -inf, n_kept 0, probs 0, logits_out -inf); logits of +inf share all the mass, and nothing else stays.
- * Weights exp((logit - max) / T) are summed as 64-bit integers, of which 1 has at most 2^62 / V of steps: sums are the same in any order.  An id
- * whose weight rounds to 0 steps is kept where the filters keep it, with probability 0, and never drawn.
+ * Weights exp((logit - max) / T) are summed as 64-bit integers, of which 1 has at most 2^62 / V of steps: sums are the same in any order.  Min-p
+ * compares what they are before that rounding (to 10^-13): an id whose weight rounds to 0 steps is kept where the filters keep it, with the
+ * probability that its logit gives, and never drawn.
  * One of probs and logits_out may be logits itself where ld == V; else none of the three may overlap.  At most 655360 ids (MIRROR_ERR_SHAPE).  One kernel, no workspace. */
 mirror_status mirror_sample(mirror_ctx* ctx, const float* logits, int64_t ld, int M, const float* temperature,
                             const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token,

@@ -140,9 +140,9 @@ struct Weigh {
         return __hiloint2double(__double2hiint(r) + (((n >> 6) + s) << 20), __double2loint(r));
     }
     // (of an id that may be kept)
+    __device__ __forceinline__ double unrounded(float l) const { return exp2_scaled<4>(y_of(l), shift, table); }
     __device__ __forceinline__ u64 operator()(float l) const {
-        const double w = exp2_scaled<4>(y_of(l), shift, table);
-        return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull;          // + 2^52: the low bits are the integer
+        return (u64)__double_as_longlong(unrounded(l) + 4503599627370496.0) & 0xfffffffffffffull;         // + 2^52: the low bits are the integer
     }
     __device__ __forceinline__ double share(float l, const double* shares) const { return exp2_scaled<3>(y_of(l), 0, shares); }
 };
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ids that may be kept: neither NaN nor -inf, and where the maximum is +inf only those
     const float least = max_inf ? INFINITY : -3.4028235e38f;
     auto may = [&](float l) { return l >= least; };
-    const u64 min_w = by_m ? (u64)fmin(ceil(min_p * p.two_s), p.two_s) : 0ull;
+    const double min_w = fmin(min_p, 1.0) * p.two_s;             // (not rounded to steps: what weighs less than one may be kept, too)
     // composite key of an id: smaller is ahead
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
     const float inv_T = 1.f / T;
@@ -697,6 +697,12 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 constexpr int P = decltype(per)::value;          // ids of a thread
                 if (P == 1) sort_short(s, n_list);
                 else sort_list<kThreads, P>(s, n_list);
+                int n_m = n_list;                                // of the ranks those that Min-p keeps
+                if (by_m) {
+                    n_m = 0;
+#pragma unroll 1
+                    for (int r = tid; r - tid < n_list; r += kThreads) n_m += __syncthreads_count(r < n_list && weigh.unrounded(logit_of(s.list[r])) >= min_w);
+                }
                 u64 key[P], w[P], sel[P], before;
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
@@ -712,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll
                 for (int j = 0; j < P; ++j) {
                     const int r = tid * P + j;
-                    const bool stays = r < n_list && (r == 0 || ((!by_k || r < k) && (!by_p || (double)before < want) && (!by_m || w[j] >= min_w)));
+                    const bool stays = r < n_list && (r == 0 || ((!by_k || r < k) && (!by_p || (double)before < want) && r < n_m));
                     kept += stays;
                     if (stays) {
                         kept_mass += w[j];
@@ -958,7 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     while (lo < hi) {
                         const uint32_t mid = lo + ((hi - lo) >> 1);
                         const float l = unkey(mid);
-                        if (l > -INFINITY && weigh(l) >= min_w) hi = mid; else lo = mid + 1;
+                        if (l > -INFINITY && weigh.unrounded(l) >= min_w) hi = mid; else lo = mid + 1;
                     }
                     if (lane == 0) s.base = ((u64)~hi << 32) | 0xffffffffull;
                 }

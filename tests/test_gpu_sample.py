@@ -281,3 +281,22 @@ def test_clusters_whose_last_ctas_have_few_ids_or_none(V, M):
     want = [int(O.sample_row(x[r], u=float(u[r]))[0]) for r in range(M)]
     got = [m.mirror_sample(xd, u)["token"] for _ in range(200)]
     assert (torch.stack(got).cpu() == torch.tensor(want, dtype=torch.int32)).all()
+
+
+@pytest.mark.parametrize("V,crowd", [(300, 300), (32000, 500), (32000, 32000), (128256, 1000), (655360, 800), (655360, 655360)])
+@pytest.mark.parametrize("M", [2, 60])
+def test_min_p_below_a_step_of_the_sums(V, crowd, M):
+    """Thresholds of 10^-12 to 10^-30, where a weight is less than one of the steps that sums are counted in, or a few of them: what stays goes
+    by the weight itself.  `crowd` ids lie up to 80 nats below the largest, the others further down."""
+    if M * V > 1 << 24:
+        M = 25                                                   # (more rows than two large CTAs an SM hold, at this size)
+    mp = np.resize(np.float32([1e-12, 1e-15, 3e-13, 1e-30, 1e-18]), M)
+    x = logits_of(M, V, V + crowd, std=1.0, leaders=0) - np.float32(200.0)
+    rng = np.random.default_rng(crowd)
+    for r in range(M):
+        x[r, rng.choice(V, crowd, replace=False)] = -rng.uniform(0.0, 80.0, crowd).astype(np.float32)
+        z = x[r].astype(np.float64) - x[r].max()
+        assert np.abs(z - np.log(float(mp[r]))).min() > 1e-9     # (no id so close to the threshold that the last bits of exp decide)
+    check(x, mp=mp, seed=V)
+    check(x[:2], p=[0.999, 1.0], mp=mp[:2], seed=V + 1)
+    check(x[:2], k=[40, 1000], mp=mp[:2], seed=V + 2)
