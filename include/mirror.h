@@ -386,7 +386,7 @@ mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mir
  *   top_k       int32 [M], nullable: the top_k largest logits stay, of equals the lower ids (<= 0 or >= V: off)
  *   top_p       fp32 [M], nullable: of what is left, the shortest front of the ranks whose share of the probability reaches
  *               top_p: a token stays iff those ahead of it have less (>= 1: off; <= 0: the first alone)
- *   min_p       fp32 [M], nullable: tokens with at least min_p times the largest probability stay (<= 0: off)
+ *   min_p       fp32 [M], nullable: tokens with at least min_p times the largest probability stay (<= 0: off; > 1: the first alone)
  *   u           fp32 [M] in [0, 1): the token is the first id at which the kept tokens' probabilities, summed over ids in
  *               increasing order, exceed u (inverse CDF, as in mirror_accept_select)
  *   token       int32 [M]; logprob fp32 [M], nullable: ln of its probability among the kept; n_kept int32 [M], nullable

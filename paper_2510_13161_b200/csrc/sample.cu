@@ -368,13 +368,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     float T = p.temperatures ? p.temperatures[row] : p.temperature;
     const bool first_only = !(T > 0.f);
     if (first_only) T = 1.f;
+    const double min_p = p.min_p && !first_only ? (double)p.min_p[row] : 0.0;
+    const bool by_m = min_p > 0.0 && min_p <= 1.0;
     int k = p.top_k ? p.top_k[row] : 0;
-    if (first_only) k = 1;
+    if (first_only || min_p > 1.0) k = 1;                        // (no id has more than the largest probability: the first alone, of equals, too)
     const bool by_k = k > 0 && k < p.V;
     const double top_p = p.top_p && !first_only ? (double)p.top_p[row] : 1.0;
     const bool by_p = top_p < 1.0;
-    const double min_p = p.min_p && !first_only ? (double)p.min_p[row] : 0.0;
-    const bool by_m = min_p > 0.0;
     const bool whole_total = by_p && !by_k;                      // Top-p of the whole row
     const bool max_inf = mx == INFINITY, none = mx == -INFINITY; // (none: nothing to keep)
     Weigh weigh;
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ids that may be kept: neither NaN nor -inf, and where the maximum is +inf only those
     const float least = max_inf ? INFINITY : -3.4028235e38f;
     auto may = [&](float l) { return l >= least; };
-    const double min_w = fmin(min_p, 1.0) * p.two_s;             // (not rounded to steps: what weighs less than one may be kept, too)
+    const double min_w = min_p * p.two_s;             // (not rounded to steps: what weighs less than one may be kept, too)
     // composite key of an id: smaller is ahead
     auto key_of = [&](float l, int id) { return ((u64)~mirror_order_key(l + 0.f) << 32) | (uint32_t)id; };      // (-0 and 0 are equal)
     const float inv_T = 1.f / T;
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         // a logit below all of the bins up to b, and one that Min-p surely leaves out
         const float slack = fabsf(weigh.hi) * 1e-6f;
         auto below_bin = [&](int b) { return b >= kBins - 1 || max_inf ? least : weigh.hi - (float)(b + 1) * T * (1.00002f / kBinsPerNat) - slack; };
-        const float below_m = by_m && !max_inf ? weigh.hi + T * (logf((float)fmin(min_p, 1.0)) * 1.00002f - 1e-5f) - slack : least;
+        const float below_m = by_m && !max_inf ? weigh.hi + T * (logf((float)min_p) * 1.00002f - 1e-5f) - slack : least;
         // Candidates: into the CTA's own list (an atomic of another CTA's memory is a trip of a thousand cycles), and once the exchange has
         // told how many every CTA has, count(c) of them, one behind the other into the leader's.
         auto gather = [&](auto count) {

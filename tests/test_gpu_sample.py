@@ -300,3 +300,15 @@ def test_min_p_below_a_step_of_the_sums(V, crowd, M):
     check(x, mp=mp, seed=V)
     check(x[:2], p=[0.999, 1.0], mp=mp[:2], seed=V + 1)
     check(x[:2], k=[40, 1000], mp=mp[:2], seed=V + 2)
+
+
+@pytest.mark.parametrize("M,V", [(3, 9), (3, 40000), (60, 40000)])
+def test_min_p_of_one_and_more(M, V):
+    """Of ids with the largest logit all have one times the largest probability, none has more: the first alone stays then."""
+    x = logits_of(M, V, V, std=0.5, leaders=0)
+    x[0, V // 3:] = 7.0
+    x[1, [2, V - 1]] = 9.0
+    for p in (None, 0.7):
+        check(x, p=p, mp=np.resize(np.float32([1.0, 1.0, 1.0, 1.0, 1.0001, np.inf, 3.0]), M), seed=V)
+        check(x, p=p, k=30000, mp=np.resize(np.float32([1.5, np.inf, 1.0001, 0.5]), M), seed=V + 1)
+        check(x, p=p, T=0.0, mp=1.5, seed=V + 2)
