@@ -355,7 +355,8 @@ mirror_status mirror_rope_init(mirror_rope* out, int head_dim, int rotary_dim, i
  *   q         bf16 [L, R, Hq, d], nullable; k, v  bf16 [L, R, Hkv, d].  Heads and elements are contiguous; rows are q_row / kv_row
  *             elements apart and layers q_layer / kv_layer (so the three may be columns of one projection's output); all of
  *             them multiples of 8
- *   q_out     bf16 [L, R, Hq, d], contiguous, nullable (with q); may be q where that is contiguous
+ *   q_out     bf16 [L, R, Hq, d], contiguous, nullable (with q); may be q where that is contiguous (MIRROR_ERR_ARG where it is not), else it
+ *             must overlap none of q, k and v
  * Angles are reduced in double precision, the rotation is fp32 with one rounding.  Two rows must not share a (page, slot).  A position
  * beyond max_pages_per_req*16 or below 0, or a page outside the pool, is skipped and reported through mirror_device_status.
  * One kernel. */

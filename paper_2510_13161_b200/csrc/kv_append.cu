@@ -215,8 +215,12 @@ extern "C" mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, 
     const int d = ctx->desc.head_dim, Hq = ctx->desc.n_q_heads, Hkv = ctx->desc.n_kv_heads;
     if (((uintptr_t)k & 15) || ((uintptr_t)v & 15) || ((uintptr_t)q & 15) || ((uintptr_t)q_out & 15)) return MIRROR_ERR_ARG;
     if (kv_row % 8 || kv_layer % 8 || (q && (q_row % 8 || q_layer % 8))) return MIRROR_ERR_SHAPE;
-    // rows (and layers) that are closer than they are long would run into one another
+    // (layers may share their rows, which are only read; rows that are closer than they are long are nobody's layout)
     if (kv_row < (int64_t)Hkv * d || (q && q_row < (int64_t)Hq * d) || kv_layer < 0 || q_layer < 0) return MIRROR_ERR_SHAPE;
+    // In place an element is read and written by one thread only where both tensors lie alike; else a row may be turned after another
+    // block has overwritten it.
+    if (q && q == q_out && ((rows->n_rows > 1 && q_row != (int64_t)Hq * d) || (kv->num_layers > 1 && q_layer != (int64_t)rows->n_rows * Hq * d)))
+        return MIRROR_ERR_ARG;
     if (rope) {
         if (rope->rotary_dim <= 0 || rope->rotary_dim > d || rope->rotary_dim % 16 != 0) return MIRROR_ERR_SHAPE;
         if (!isfinite(rope->amplitude)) return MIRROR_ERR_ARG;

@@ -181,3 +181,24 @@ def test_refusals():
     for value in (0, 24, 80):
         bad.rotary_dim = value
         assert code(rows, rope=C.byref(bad)) == 2
+
+
+def test_in_place_only_where_the_queries_are_contiguous():
+    m = make(4, 2, 64)
+    import ctypes as C
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    table, lens = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    k, q = torch.zeros((2, 8, 2, 64), **bf), torch.zeros((2, 16, 4, 64), **bf)
+
+    def code(L, R, q_row, q_layer, q_out=None):
+        pools = [torch.zeros((L, 4, 2, PAGE, 64), **bf) for _ in range(2)]
+        kv, rows = m.kv(*pools, table, lens), m.rows(None, R, R, 1)
+        got = m.lib.mirror_kv_append(m._ctx, C.byref(kv), C.byref(rows), None, q.data_ptr(), q_row, q_layer, q.data_ptr() if q_out is None else q_out,
+                                     k.data_ptr(), k.data_ptr(), 128, 1024, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        return got
+    assert code(2, 8, 256, 2048) == 0 and code(1, 8, 256, 0) == 0 and code(2, 1, 512, 256) == 0
+    other = torch.empty((2, 8, 4, 64), **bf).data_ptr()
+    for L, R, q_row, q_layer in ((1, 8, 512, 0), (2, 8, 256, 4096), (2, 8, 256, 0), (2, 8, 512, 4096), (2, 1, 256, 512)):
+        assert code(L, R, q_row, q_layer) == 1
+        assert code(L, R, q_row, q_layer, other) == 0              # (the same queries, out of place)
