@@ -317,7 +317,7 @@ mirror_status mirror_kv_commit_fp8(mirror_ctx* ctx, const mirror_kv* kv, const m
 typedef struct {
     int batch;                /* B requests, at most 1024 */
     int n_rows;               /* R: rows of the tensors, those behind the last request's included (they are left as they are) */
-    int max_rows;             /* upper bound of a request's rows; 1: single tokens */
+    int max_rows;             /* upper bound of a request's rows; 1: single tokens.  Rows beyond it are reported, and left as they are */
     const int32_t* row_start; /* device [B + 1], not decreasing (where it does, mirror_attn_causal reports it, and its output is not defined):
                                  request b has the rows row_start[b] .. row_start[b+1] - 1;
                                  NULL: every request has max_rows rows (R >= B * max_rows) */
@@ -357,8 +357,9 @@ mirror_status mirror_rope_init(mirror_rope* out, int head_dim, int rotary_dim, i
  *             them multiples of 8
  *   q_out     bf16 [L, R, Hq, d], contiguous, nullable (with q); may be q where that is contiguous (MIRROR_ERR_ARG where it is not), else it
  *             must overlap none of q, k and v
- * Angles are reduced in double precision, the rotation is fp32 with one rounding.  Two rows must not share a (page, slot).  A position
- * beyond max_pages_per_req*16 or below 0, or a page outside the pool, is skipped and reported through mirror_device_status.
+ * Angles are reduced in double precision, the rotation is fp32 with one rounding.  Two rows must not share a (page, slot).  Keys and values
+ * of a position beyond max_pages_per_req*16 or below 0, or of a page outside the pool, are skipped and reported through
+ * mirror_device_status (their queries are turned all the same: a position below 0 as 0); so are rows beyond max_rows, queries included.
  * One kernel. */
 mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, const mirror_rows* rows, const mirror_rope* rope,
                                const void* q, int64_t q_row, int64_t q_layer, void* q_out, const void* k, const void* v,

@@ -80,6 +80,10 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
         if (row < p.R) {
             if (p.row_start) {
                 b = request_of(p.row_start, p.B, row, &first);
+                if (b >= 0 && row - first >= p.max_rows) {     // (mirror_attn_causal would not see it)
+                    if (lane == 0) report(p.status, 830);
+                    b = -1;
+                }
             } else if (row / p.max_rows < p.B) {
                 b = row / p.max_rows;
                 first = b * p.max_rows;

@@ -202,3 +202,23 @@ def test_in_place_only_where_the_queries_are_contiguous():
     for L, R, q_row, q_layer in ((1, 8, 512, 0), (2, 8, 256, 4096), (2, 8, 256, 0), (2, 8, 512, 4096), (2, 1, 256, 512)):
         assert code(L, R, q_row, q_layer) == 1
         assert code(L, R, q_row, q_layer, other) == 0              # (the same queries, out of place)
+
+
+def test_rows_beyond_max_rows_are_reported_and_skipped():
+    """As mirror_attn_causal does: what it would not see is not appended."""
+    m = make(2, 2, 64)
+    k, q = (torch.randn((1, 9, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2))
+    pools = [torch.zeros((1, 4, 2, PAGE, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    kv = m.kv(*pools, torch.tensor([[0, 1], [2, 3]], dtype=torch.int32, device="cuda"), torch.tensor([14, 0], dtype=torch.int32, device="cuda"))
+    start = torch.tensor([0, 5, 8], dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 7.0)
+    m.mirror_kv_append(kv, m.rows(start, 9, 3), k, k, q=q, q_out=out)
+    torch.cuda.synchronize()
+    assert m.device_status() == (6, 830)
+    v = pools[1][0]
+    assert torch.equal(v[0, :, 14:].transpose(0, 1), k[0, :2]) and torch.equal(v[1, :, :1].transpose(0, 1), k[0, 2:3])
+    assert torch.equal(v[2, :, :3].transpose(0, 1), k[0, 5:8]) and int((pools[1] != 0).any(-1).any(2).sum()) == 6
+    assert torch.equal(out[0, [0, 1, 2, 5, 6, 7]], q[0, [0, 1, 2, 5, 6, 7]]) and (out[0, [3, 4, 8]] == 7.0).all()
+    m.mirror_kv_append(kv, m.rows(start, 9, 5), k, k, q=q, q_out=out)
+    torch.cuda.synchronize()
+    assert m.device_status() == (0, 0) and torch.equal(out[0, :8], q[0, :8])
