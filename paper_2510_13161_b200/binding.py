@@ -240,6 +240,8 @@ class Mirror:
         self._heads, self._vocab = (n_q_heads, n_kv_heads, head_dim), vocab
         self._rows_need = None
         self._ws = None
+        self._ws_captured = False    # a call that uses it lies in a captured graph
+        self._old_ws = []            # such workspaces that larger ones have taken the place of
         self._need = {}              # workspace bytes by (what, batch, nodes): they depend on nothing else
         self._keep = []
 
@@ -282,23 +284,35 @@ class Mirror:
                                                what, C.byref(out)), "mirror_workspace_bytes")
         return out.value
 
-    def ensure_workspace(self, tree: Tree, kv: Optional[KV], what: int):
+    def _use_workspace(self, need: int, stream=None):
+        """A workspace of at least `need` bytes for a call on `stream`.  One that a captured call uses stays alive when a larger one takes its
+        place (its graph goes on writing there); another is given back once the stream is through with it."""
+        if self._ws is None or self._ws.numel() < need:
+            if self._ws is not None:
+                if self._ws_captured:
+                    self._old_ws.append(self._ws)
+                else:
+                    self._ws.record_stream(stream if stream is not None else torch.cuda.current_stream(self.device))
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self._ws_captured = False
+            _check(self.lib.mirror_set_workspace(self._ctx, C.c_void_p(self._ws.data_ptr()), need), "mirror_set_workspace")
+        if not self._ws_captured and torch.cuda.is_current_stream_capturing():
+            self._ws_captured = True
+
+    def ensure_workspace(self, tree: Tree, kv: Optional[KV], what: int, stream=None):
         key = (what, tree.batch, tree.n_nodes)
         need = self._need.get(key)
         if need is None:
             need = self.workspace_bytes(tree, kv, what)
             if len(self._need) < 4096:
                 self._need[key] = need
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            _check(self.lib.mirror_set_workspace(self._ctx, C.c_void_p(self._ws.data_ptr()), need),
-                   "mirror_set_workspace")
+        self._use_workspace(need, stream)
 
     # ---- entry points -----------------------------------------------------------------------
     def mirror_attn_verify(self, kv: KV, tree: Tree, q, k_new, v_new, out=None, lse_out=None, stream=None):
         if out is None:
             out = torch.empty_like(q)
-        self.ensure_workspace(tree, kv, WS_ATTN)
+        self.ensure_workspace(tree, kv, WS_ATTN, stream)
         _check(self.lib.mirror_attn_verify(self._ctx, C.byref(kv), C.byref(tree), _ptr(q, torch.bfloat16, "q"),
                                            _ptr(k_new, torch.bfloat16, "k_new"), _ptr(v_new, torch.bfloat16, "v_new"),
                                            _ptr(out, torch.bfloat16, "out"), _ptr(lse_out, torch.float32, "lse_out"),
@@ -342,7 +356,7 @@ class Mirror:
                                lse_out=None, stream=None):
         if out is None:
             out = torch.empty_like(q)
-        self.ensure_workspace(tree, kv, WS_ATTN)
+        self.ensure_workspace(tree, kv, WS_ATTN, stream)
         _check(self.lib.mirror_attn_verify_fp8(self._ctx, C.byref(kv), C.byref(tree), _ptr(q, torch.bfloat16, "q"),
                                                _ptr(k_new8, torch.uint8, "k_new8"), _ptr(v_new8, torch.uint8, "v_new8"),
                                                _ptr(k_scale, torch.float32, "k_scale"), _ptr(v_scale, torch.float32, "v_scale"),
@@ -368,7 +382,7 @@ class Mirror:
             res["logits"] = torch.empty((M, self.desc.vocab), dtype=torch.float32, device=dev)
         t = Tree(1, M if M <= 128 else 128, 0, 0, None, None)
         t.batch, t.n_nodes = (M + 127) // 128, min(M, 128)      # sizes only: batch * n_nodes >= M
-        self.ensure_workspace(t, None, WS_LMHEAD_TOPK if topk else WS_LMHEAD)
+        self.ensure_workspace(t, None, WS_LMHEAD_TOPK if topk else WS_LMHEAD, stream)
         _check(self.lib.mirror_lmhead_reduce(self._ctx, _ptr(hidden, torch.bfloat16, "hidden"), M,
                                              _ptr(W, torch.bfloat16, "W"), topk,
                                              _ptr(gather_row, torch.int32, "gather_row"),
@@ -395,7 +409,7 @@ class Mirror:
                    logits=torch.empty((M, self.desc.vocab), dtype=torch.float32, device=dev) if want_logits else None)
         t = Tree(1, M if M <= 128 else 128, 0, 0, None, None)
         t.batch, t.n_nodes = (M + 127) // 128, min(M, 128)      # sizes only: batch * n_nodes >= M
-        self.ensure_workspace(t, None, WS_LMHEAD)
+        self.ensure_workspace(t, None, WS_LMHEAD, stream)
         _check(self.lib.mirror_lmhead_reduce_fp8(self._ctx, _ptr(hidden8, torch.uint8, "hidden8"), _ptr(h_scale, torch.float32, "h_scale"),
                                                  M, _ptr(W8, torch.uint8, "W8"), _ptr(w_scale, torch.float32, "w_scale"),
                                                  _ptr(res["argmax"]), _ptr(res["maxlogit"]), _ptr(res["lse"]), _ptr(res["logits"]),
@@ -419,7 +433,7 @@ class Mirror:
         lp = torch.empty((M, kappa), dtype=torch.bfloat16, device=hidden_le.device)
         t = Tree(1, M if M <= 128 else 128, 0, 0, None, None)
         t.batch, t.n_nodes = (M + 127) // 128, min(M, 128)      # sizes only: batch * n_nodes >= M
-        self.ensure_workspace(t, None, WS_LMHEAD_TOPK)
+        self.ensure_workspace(t, None, WS_LMHEAD_TOPK, stream)
         _check(self.lib.mirror_early_exit_tap(self._ctx, _ptr(hidden_le, torch.bfloat16, "hidden_le"), M,
                                               _ptr(W, torch.bfloat16, "W"), kappa, _ptr(ids, torch.int32, "msg_ids"),
                                               _ptr(lp, torch.bfloat16, "msg_logprob"), _stream(stream)), "mirror_early_exit_tap")
@@ -523,9 +537,7 @@ class Mirror:
             n = C.c_size_t()
             _check(self.lib.mirror_rows_workspace_bytes(self._ctx, C.byref(rows), C.byref(n)), "mirror_rows_workspace_bytes")
             need = self._rows_need = n.value
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-            _check(self.lib.mirror_set_workspace(self._ctx, C.c_void_p(self._ws.data_ptr()), need), "mirror_set_workspace")
+        self._use_workspace(need, stream)
         _check(self.lib.mirror_attn_causal(self._ctx, C.byref(kv), C.byref(rows), window, sinks, _ptr(q, torch.bfloat16, "q"),
                                            _ptr(out, torch.bfloat16, "out"), _ptr(lse_out, torch.float32, "lse_out"), _stream(stream)),
                "mirror_attn_causal")
@@ -625,7 +637,7 @@ class Mirror:
             e = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device=self.device)
             out = dict(q=e(L, B, n, Hq, d), k_new=e(L, B, n, Hkv, d), v_new=e(L, B, n, Hkv, d), attn_out=e(L, B, n, Hq, d),
                        x_out=torch.empty_like(x), hidden=torch.empty_like(x))
-        self.ensure_workspace(tree, kv, WS_ATTN)
+        self.ensure_workspace(tree, kv, WS_ATTN, stream)
         _check(self.lib.mirror_target_forward(self._ctx, C.byref(target), C.byref(kv), C.byref(tree), _ptr(x, torch.bfloat16, "x"),
                                               _ptr(out["q"]), _ptr(out["k_new"]), _ptr(out["v_new"]), _ptr(out["attn_out"]),
                                               _ptr(out["x_out"]), _ptr(out["hidden"]), _ptr(scratch), scratch.numel(),
@@ -646,7 +658,7 @@ class Mirror:
         out = dict(q=e(L, B, n, Hq, d), k_new=e(L, B, n, Hkv, d), v_new=e(L, B, n, Hkv, d), k_new8=e8(L, B, n, Hkv, d),
                    v_new8=e8(L, B, n, Hkv, d), attn_out=e(L, B, n, Hq, d), x_out=torch.empty_like(x), hidden=torch.empty_like(x))
         qs = (C.c_float * L)(*[float(v) for v in q_scales])
-        self.ensure_workspace(tree, kv, WS_ATTN)
+        self.ensure_workspace(tree, kv, WS_ATTN, stream)
         _check(self.lib.mirror_target_forward_fp8(self._ctx, C.byref(target), C.byref(kv), C.byref(tree), _ptr(x, torch.bfloat16, "x"),
                                                   _ptr(k_scale, torch.float32, "k_scale"), _ptr(v_scale, torch.float32, "v_scale"), qs,
                                                   _ptr(out["q"]), _ptr(out["k_new"]), _ptr(out["v_new"]), _ptr(out["k_new8"]),
@@ -662,7 +674,7 @@ class Mirror:
         if out is None:
             out = AcceptResult(tree.batch, tree.gamma, self.device)
         if tree_scratch:
-            self.ensure_workspace(tree, None, WS_STEP_TREE)
+            self.ensure_workspace(tree, None, WS_STEP_TREE, stream)
         o = out.struct()
         _check(self.lib.mirror_accept_select(self._ctx, C.byref(tree), C.byref(acc), C.byref(o), _stream(stream)),
                "mirror_accept_select")
@@ -678,7 +690,7 @@ class Mirror:
                 raise ValueError(f"{name} must be a contiguous host tensor of {dtype}")
             return C.c_void_p(t.data_ptr())
         ho = AcceptHostOut(*[(C.c_void_p(h_out[f].data_ptr()) if h_out and f in h_out else None) for f, _ in AcceptHostOut._fields_])
-        self.ensure_workspace(tree, kv, {ACCEPT_GREEDY: WS_STEP_GREEDY, ACCEPT_SPEC_TREE: WS_STEP_TREE}.get(acc.mode, WS_STEP_SPEC))
+        self.ensure_workspace(tree, kv, {ACCEPT_GREEDY: WS_STEP_GREEDY, ACCEPT_SPEC_TREE: WS_STEP_TREE}.get(acc.mode, WS_STEP_SPEC), stream)
         o = out.struct()
         _check(self.lib.mirror_verify_step_host(self._ctx, C.byref(kv), C.byref(tree), hp(h_in["q"], torch.bfloat16, "q"),
                                                 hp(h_in["k_new"], torch.bfloat16, "k_new"), hp(h_in["v_new"], torch.bfloat16, "v_new"),
@@ -693,7 +705,7 @@ class Mirror:
                            out: Optional[AcceptResult] = None, argmax_out=None, stream=None) -> AcceptResult:
         if out is None:
             out = AcceptResult(tree.batch, tree.gamma, self.device)
-        self.ensure_workspace(tree, kv, {ACCEPT_GREEDY: WS_STEP_GREEDY, ACCEPT_SPEC_TREE: WS_STEP_TREE}.get(acc.mode, WS_STEP_SPEC))
+        self.ensure_workspace(tree, kv, {ACCEPT_GREEDY: WS_STEP_GREEDY, ACCEPT_SPEC_TREE: WS_STEP_TREE}.get(acc.mode, WS_STEP_SPEC), stream)
         o = out.struct()
         _check(self.lib.mirror_verify_step(self._ctx, C.byref(kv), C.byref(tree), _ptr(q, torch.bfloat16, "q"),
                                            _ptr(k_new, torch.bfloat16, "k_new"), _ptr(v_new, torch.bfloat16, "v_new"),
@@ -708,7 +720,7 @@ class Mirror:
         """mirror_verify_step over an e4m3 cache (kv from kv_fp8; k_new8 / v_new8 uint8 codes under the cache's scales)."""
         if out is None:
             out = AcceptResult(tree.batch, tree.gamma, self.device)
-        self.ensure_workspace(tree, kv, {ACCEPT_GREEDY: WS_STEP_GREEDY, ACCEPT_SPEC_TREE: WS_STEP_TREE}.get(acc.mode, WS_STEP_SPEC))
+        self.ensure_workspace(tree, kv, {ACCEPT_GREEDY: WS_STEP_GREEDY, ACCEPT_SPEC_TREE: WS_STEP_TREE}.get(acc.mode, WS_STEP_SPEC), stream)
         o = out.struct()
         _check(self.lib.mirror_verify_step_fp8(self._ctx, C.byref(kv), C.byref(tree), _ptr(q, torch.bfloat16, "q"),
                                                _ptr(k_new8, torch.uint8, "k_new8"), _ptr(v_new8, torch.uint8, "v_new8"),

@@ -168,3 +168,30 @@ def test_the_whole_chain_captured_and_replayed():
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(a, want_a) and torch.equal(got["token"], want["token"]) and m.device_status() == (0, 0)
+
+
+def test_a_captured_call_after_the_workspace_has_grown():
+    """A graph's attention keeps the workspace that it was captured with when a later call needs a larger one: its replay is right, and
+    writes into nothing that was allocated since."""
+    hq, hkv, d, n = 8, 2, 128, 30
+    m = make(hq, hkv, d, vocab=30000)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    bf = lambda *s: torch.randn(s, device="cuda", generator=g).to(torch.bfloat16)  # noqa: E731
+    k_pool, v_pool, table = cache(1, 1, 200, hkv, d)
+    k_pool.copy_(bf(*k_pool.shape)), v_pool.copy_(bf(*v_pool.shape))
+    kv, rows, q = m.kv(k_pool, v_pool, table, torch.tensor([3000], dtype=torch.int32, device="cuda")), m.rows(None, n, n, 1), bf(1, n, hq, d)
+    want = m.mirror_attn_causal(kv, rows, q)                     # (one request over 3030 tokens: its unit is cut, records are written)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = m.mirror_attn_causal(kv, rows, q)
+    before = m._ws.data_ptr(), m._ws.numel()
+    m.mirror_lmhead_reduce(bf(300, 256), bf(30000, 256))
+    assert m._ws.numel() > before[1]
+    torch.cuda.synchronize()
+    others = [torch.full((before[1],), 7, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    assert all(t.data_ptr() != before[0] for t in others)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all((t == 7).all() for t in others) and m.device_status() == (0, 0)
