@@ -195,3 +195,96 @@ def test_a_captured_call_after_the_workspace_has_grown():
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(got, want) and all((t == 7).all() for t in others) and m.device_status() == (0, 0)
+
+
+def test_one_cache_from_the_prompt_through_a_verify_step_and_on():
+    """A model of one layer (Q, K, V and logits by way of its tokens' rows of a table) over one cache: two prompts, single tokens without
+    a draft, a drafted chain with its distributions, mirror_verify_step of that chain, mirror_kv_commit, and a token more.  The draft is the
+    target, so all of it is accepted (u <= 0.8, and p and q differ by the roundings of P alone); what the cache then holds is what
+    one prompt of the whole sequence leaves, bit for bit, and the last row's attention is that prompt's to the roundings of P and the output."""
+    hq, hkv, d, V, B, gamma = 4, 2, 64, 3000, 2, 4
+    H = hq * d
+    m = make(hq, hkv, d, vocab=V)
+    g = torch.Generator(device="cuda").manual_seed(17)
+    bf = lambda *s, std=1.0: (torch.randn(s, device="cuda", generator=g) * std).to(torch.bfloat16)  # noqa: E731
+    qkv_of = m.mirror_linear(bf(V, H), bf((hq + 2 * hkv) * d, H, std=H ** -0.5)).view(V, hq + 2 * hkv, d)
+    W, rope = bf(V, H, std=0.1), m.rope(theta=1e4)
+    k_pool, v_pool, table = cache(1, B, 6, hkv, d)
+    lens = [37, 9]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    done = torch.zeros(B, **i32)
+    seq = [torch.randint(0, V, (n,), device="cuda", generator=g).tolist() for n in lens]
+
+    def forward(tokens, pools=None, at=None):
+        """Appends ragged tokens, attends; -> (turned queries, attention) [1, R, hq, d]."""
+        start = np.concatenate([[0], np.cumsum([len(t) for t in tokens])]).astype(np.int32)
+        x = qkv_of[torch.tensor(sum(tokens, []), device="cuda")].unsqueeze(0)
+        kv = m.kv(*(pools or (k_pool, v_pool)), table, done if at is None else at)
+        rows = m.rows(torch.from_numpy(start).cuda(), int(start[-1]), max(len(t) for t in tokens))
+        q = m.mirror_kv_append(kv, rows, x[:, :, hq:hq + hkv], x[:, :, hq + hkv:], q=x[:, :, :hq], rope=rope)
+        return q, m.mirror_attn_causal(kv, rows, q)
+
+    def draw(a, temperature, p=1.0):
+        logits = m.mirror_lmhead_reduce(a.reshape(B, H).contiguous(), W, want_logits=True)["logits"]
+        f = lambda x: torch.full((B,), x, device="cuda")  # noqa: E731
+        return m.mirror_sample(logits, torch.rand(B, device="cuda", generator=g), temperature=f(temperature), top_p=f(p), want_probs=True)
+
+    # the prompts, and three tokens without a draft (the last of them stays out of the cache: the tree's root)
+    _, a = forward(seq)
+    a = a[0, torch.tensor(np.cumsum(lens) - 1, device="cuda")]
+    done += torch.tensor(lens, **i32)
+    for step in range(3):
+        new = draw(a, 0.8, 0.9)["token"].tolist()
+        for b in range(B):
+            seq[b].append(new[b])
+        if step < 2:
+            _, a = forward([[t] for t in new])
+            done += 1
+    # the draft: it continues in the pages behind the cache's tokens, which are not counted
+    root, chain, probs, qs, at = new, [], [], [], done.clone()
+    for i in range(gamma + 1):
+        q, a = forward([[t] for t in (root if i == 0 else chain[-1])], at=at)
+        qs.append(q.view(1, B, 1, hq, d))
+        at += 1
+        if i < gamma:
+            s = draw(a, 1.0)
+            chain.append(s["token"].tolist())
+            probs.append(s["probs"])
+    where = (done[:, None] + torch.arange(gamma + 1, device="cuda")).long()                    # the nodes' positions
+    pages, slots = table.long().gather(1, where // PAGE), where % PAGE
+    k_new, v_new = (pool[:, pages, :, slots].permute(2, 0, 1, 3, 4).contiguous() for pool in (k_pool, v_pool))
+    assert k_new.shape == (1, B, gamma + 1, hkv, d)
+    for pool in (k_pool, v_pool):
+        pool[:, pages, :, slots] = 100.0                         # (a verify step that read the draft's rows would be far off)
+    tokens = torch.tensor([root] + chain, **i32).t().contiguous()
+    tree, kv = m.tree(tokens, 1, gamma), m.kv(k_pool, v_pool, table, done)
+    acc = m.accept_in(binding.ACCEPT_SPEC_SAMPLING, True, q_probs=torch.stack(probs, 1).contiguous(),
+                      u_accept=torch.rand((B, gamma + 1), device="cuda", generator=g) * 0.8, u_resample=torch.rand((B, gamma + 1), device="cuda", generator=g))
+    attn = torch.empty((1, B, gamma + 1, hq, d), dtype=torch.bfloat16, device="cuda")
+    res = m.mirror_verify_step(kv, tree, torch.cat(qs, 2).contiguous(), k_new, v_new, None, W, acc, attn)
+    m.mirror_kv_commit(kv, tree, k_new, v_new, res, done)
+    torch.cuda.synchronize()
+    assert m.device_status() == (0, 0)
+    got = res.cpu()
+    assert got["n_accepted"].tolist() == [gamma] * B and got["n_emitted"].tolist() == [gamma + 1] * B
+    assert got["emitted"][:, :gamma].tolist() == [[chain[i][b] for i in range(gamma)] for b in range(B)]
+    assert done.tolist() == [n + 3 + gamma for n in lens]
+    for b in range(B):
+        seq[b] += got["emitted"][b].tolist()
+    # a token more, and the whole sequence as one prompt
+    _, a = forward([[s[-1]] for s in seq])
+    pools, zero = tuple(torch.zeros_like(p) for p in (k_pool, v_pool)), torch.zeros(B, **i32)
+    _, want = forward(seq, pools, zero)
+    torch.cuda.synchronize()
+    assert m.device_status() == (0, 0)
+    ends = np.cumsum([len(s) for s in seq])
+    for b, s in enumerate(seq):
+        assert len(s) == lens[b] + 4 + gamma and int(done[b]) == len(s) - 1
+        for i in range(len(s)):
+            for pool, whole in zip((k_pool, v_pool), pools):
+                assert torch.equal(pool[:, table[b, i // PAGE], :, i % PAGE], whole[:, table[b, i // PAGE], :, i % PAGE]), (b, i)
+    v_most = float(pools[1].abs().max())
+    near = lambda x, y: ((x.double() - y.double()).abs() <= 2 * 2.0 ** -8 * y.double().abs() + (2 * 2.0 ** -8 + 1e-5) * v_most).all()  # noqa: E731
+    assert near(a[0], want[0, torch.tensor(ends - 1, device="cuda")])
+    for b in range(B):                                           # (the verify step's rows are that prompt's, too)
+        assert near(attn[0, b], want[0, ends[b] - 2 - gamma:ends[b] - 1])
