@@ -80,10 +80,6 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
         if (row < p.R) {
             if (p.row_start) {
                 b = request_of(p.row_start, p.B, row, &first);
-                if (b >= 0 && row - first >= p.max_rows) {     // (mirror_attn_causal would not see it)
-                    if (lane == 0) report(p.status, 830);
-                    b = -1;
-                }
             } else if (row / p.max_rows < p.B) {
                 b = row / p.max_rows;
                 first = b * p.max_rows;
@@ -93,13 +89,15 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const __grid_consta
             int pos = -1;
             long long slot = -1;
             if (b >= 0) {
-                const long long at = (long long)p.prefix_len[b] + (row - first);
-                if (at >= 0 && at < (long long)p.max_pages * 16) {
-                    const int page = p.page_table[(size_t)b * p.max_pages + (size_t)(at / 16)];
+                // (32 bits: with 64 the kernel takes 37 registers instead of 31, and prompts of 11 k rows 85 us instead of 82)
+                const int i = row - first, at = (int)min((long long)p.prefix_len[b] + i, 0x7fffffffll);
+                const bool within = i < p.max_rows;              // (mirror_attn_causal sees no others)
+                if (within && at >= 0 && at < 0x7fffffff && at / 16 < p.max_pages) {
+                    const int page = p.page_table[(size_t)b * p.max_pages + at / 16];
                     if (page >= 0 && page < p.num_pages) slot = ((long long)page * p.Hkv * 16 + at % 16) * p.d;
                 }
-                if (slot < 0) report(p.status, 820);
-                pos = (int)max(0ll, min(at, 0x7fffffffll));
+                if (slot < 0) report(p.status, within ? 820 : 830);
+                pos = within ? max(at, 0) : -1;
             }
             s_pos[warp] = pos;
             s_slot[warp] = slot;
