@@ -333,7 +333,9 @@ typedef enum {
 } mirror_rope_scaling;
 
 /* A rotation of the first rotary_dim elements of a head (the others pass through): pair i turns by position * f_i.  Pairs are
- * (i, i + rotary_dim / 2), or (2i, 2i + 1) when interleaved.  Filled by mirror_rope_init. */
+ * (i, i + rotary_dim / 2), or (2i, 2i + 1) when interleaved.  Filled by mirror_rope_init.
+ * mirror_target_forward turns a tree's nodes by plain frequencies over the whole head, in half pairs, alone; no call
+ * turns nodes in another way, so for a cache under another rotation the caller brings q and k_new to mirror_attn_verify or mirror_verify_step turned. */
 typedef struct {
     int rotary_dim;
     int interleaved;
@@ -372,12 +374,16 @@ mirror_status mirror_kv_append(mirror_ctx* ctx, const mirror_kv* kv, const mirro
  *   lse_out   fp32 [L, R, Hq], nullable: natural-log softmax denominator
  *   out may be q
  * Pages that hold no visible token are not touched (their table entries may be anything), and what lies in a touched page beside
- * the tokens that some row of its request sees may be anything, infinities and NaN included.
+ * the tokens that some row of its request sees may be anything, infinities and NaN included.  A key that is not finite concerns the rows
+ * that see it alone; a VALUE that is not finite can make rows of its request NaN that do not see it, too (their weight of 0 times it).  A
+ * row whose softmax has no value (a NaN or +inf among its scores, or nothing but -inf) is NaN.
+ * Precision: products and sums in fp32.  Requests of few rows multiply V by the weights in 16 bits (two bf16), so that the output carries its
+ * own rounding alone; longer ones by the weights rounded to bf16 once, as mirror_attn_verify does: off by up to 2^-8 sum_j w_j |v_j| more.
  * Needs a workspace of mirror_rows_workspace_bytes().  Requests of few rows (max_rows * Hq / Hkv <= 16) stream the cache through
  * warps; longer ones run on the tensor cores in tiles of 128 rows.  Rows whose positions lie beyond max_pages_per_req*16 are
  * left as they are and reported through mirror_device_status, as are requests of a length below 0 and all rows of a call whose keys, over
  * layers, heads and requests, make more tiles of 128 than 31 bits count; a page outside the pool is reported, and its tokens are read as
- * page 0's. */
+ * page 0's.  Longer requests: L * R below 2^31 (MIRROR_ERR_SHAPE). */
 mirror_status mirror_rows_workspace_bytes(const mirror_ctx* ctx, const mirror_rows* rows, size_t* bytes);
 mirror_status mirror_attn_causal(mirror_ctx* ctx, const mirror_kv* kv, const mirror_rows* rows, int window, int n_sink,
                                  const void* q, void* out, float* lse_out, void* stream);

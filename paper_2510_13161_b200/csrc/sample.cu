@@ -21,10 +21,12 @@
 //   4' otherwise only the bin in which the front ends goes to the leader; what lies ahead of it is counted and summed by all.  (A bin
 //      of more than kList ids, many equal logits above all, is bisected by key, with exact counts and masses of each half.)
 //   5  the drawn token, by the warps' masses, and the filtered distribution
-// What bounds it: double-precision arithmetic (14 operations an id, 64 a cycle and SM) where Top-p or a draw takes the whole row, the
-// bytes otherwise; for a row alone the cluster's barriers and code that runs once.  Measured on a B200: one row of 152064 ids under all
-// three filters 14.8 us (0.1 us of bytes); 64 rows x 128256 under Top-p 0.9, probabilities written, 93 us; 520 rows x 128256 under Top-k 1000
-// and Top-p 0.98, logits written, 179 us (3.0 TB/s).
+// What bounds it: where Top-p or a draw takes the whole row, instructions (147 an id, a thread each, over all passes) that leave at 42% of the
+// issue slots, and barriers, a third of the stalls: CTAs of a cluster wait for the leading one, and one row's steps hide behind three others' at
+// most.  The double-precision pipe is busy for 9% of the time only.  Where Top-k goes ahead, the leader's ranking; for a row alone the cluster's
+// barriers and code that runs once.  Both instances have 64 registers a thread and spill (900 and 540 bytes of loads in all of the code).
+// Measured on a B200: one row of 152064 ids under all three filters 15 us (0.1 us of bytes); 64 rows x 128256 under Top-p 0.9,
+// probabilities written, 97 to 101 us; 520 rows x 128256 under Top-k 1000 and Top-p 0.98, logits written, 180 us (3.0 TB/s).
 #include <cooperative_groups.h>
 #include <math.h>
 
