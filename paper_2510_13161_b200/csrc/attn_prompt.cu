@@ -176,6 +176,7 @@ __device__ __noinline__ void next_segment(Segment& s, const PromptParams& p, con
 // It is made twice as far as its inputs are concerned: ahead of the kernel in front, from whatever the lengths are then (nothing but this
 // CTA's shared memory is written), and once that kernel is through the lengths are read again: hardly ever has one changed, and then the
 // plan is made anew.  (It takes 4 us, most of them for code that runs once.)
+
 // Tiles, inclusive over the block.  (A page table has at most 2^26 entries, a pair at most 2^23 tiles: those of a block fit 32 bits.)
 __device__ uint32_t block_scan(uint32_t v, uint32_t* s_warp, uint32_t* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
